@@ -42,7 +42,8 @@ typedef enum {
   LITE_ATTN_EHIP = -5,         /* a HIP runtime call failed; lite_attn_last_hip_error() has its code */
   LITE_ATTN_ESHARED = -6,      /* refused because scratch is shared: lite_attn_set_stream on a handle of a context with
                                   any stream but the context's; lite_attn_ctx_free while handles are attached */
-  LITE_ATTN_ESCRATCH = -7      /* lite_attn_fwd_static: the shape needs more than LITE_ATTN_STATIC_SCRATCH_BYTES */
+  LITE_ATTN_ESCRATCH = -7,     /* lite_attn_fwd_static: the shape needs more than LITE_ATTN_STATIC_SCRATCH_BYTES */
+  LITE_ATTN_EWORKSPACE = -8    /* lite_attn_layer.h: the caller's workspace is missing, too small or not aligned */
 } lite_attn_error;
 
 /* desc.flags.  The skip predicate compares a tile with the running row maximum over the tiles visited BEFORE it, so

@@ -571,6 +571,7 @@ const char* lite_attn_strerror(int code) {
       return "not allowed while scratch is shared (a handle of a context runs on the context's stream; a context "
              "with live handles cannot be freed)";
     case LITE_ATTN_ESCRATCH: return "the shape needs more scratch than the static device array holds";
+    case LITE_ATTN_EWORKSPACE: return "workspace missing, too small or not 16-byte aligned";
     default: return "unknown error";
   }
 }

@@ -1,0 +1,1124 @@
+// gfx950 kernels of include/lite_attn_layer.h and its entry points.
+//
+//   rotary_kernel          : q and k -> normalised, turned, laid out anew; backwards the gradients of that, and sums for the
+//                            weights
+//   residual_fwd_kernel    : stream + gate * norm(branch) -> stream, and its norm, scaled and shifted
+//   residual_bwd_kernel    : the gradients, and per share of rows three sums for gate, scale, shift and the weights
+//   sum_rows_kernel, group_sums_kernel, weight_sums_kernel : the shares' sums, in one fixed order
+//
+// All of them move some bytes for each of a few operations: they are bound by memory, and everything here serves to keep
+// enough bytes in flight and to do nothing twice.  A row is read once: its entries stay in the registers of a team of threads,
+// eight each, until its statistics are known.  A team takes a share of consecutive rows, asks for the next row before it works
+// on this one, and keeps what belongs to its columns -- weights, gate, scale, shift, sums over tokens -- in registers all the
+// while.  Sums over a row go through DPP inside a wave and once through LDS between waves.
+#include <hip/hip_runtime.h>
+#include <stdint.h>
+
+#include "lite_attn_kernels.h"
+#include "lite_attn_layer_kernels.h"
+
+namespace la {
+namespace {
+
+typedef unsigned int u32x2 __attribute__((ext_vector_type(2)));
+typedef unsigned int u32x4 __attribute__((ext_vector_type(4)));
+typedef float f32x2 __attribute__((ext_vector_type(2)));
+
+typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+typedef _Float16 f16x2 __attribute__((ext_vector_type(2)));
+
+// Element types: two of them as they lie in a word of memory (F32: one), and the word of two values, each rounded once.
+struct Bf16 {
+  typedef __bf16 type;
+  static __device__ __forceinline__ f32x2 widen(uint32_t w) { return f32x2{__uint_as_float(w << 16), __uint_as_float(w & 0xffff0000u)}; }
+  static __device__ __forceinline__ uint32_t narrow(float a, float b) {
+    return __builtin_bit_cast(uint32_t, __builtin_convertvector(f32x2{a, b}, bf16x2));
+  }
+};
+struct F16 {
+  typedef _Float16 type;
+  static __device__ __forceinline__ f32x2 widen(uint32_t w) { return __builtin_convertvector(__builtin_bit_cast(f16x2, w), f32x2); }
+  static __device__ __forceinline__ uint32_t narrow(float a, float b) {
+    return __builtin_bit_cast(uint32_t, __builtin_convertvector(f32x2{a, b}, f16x2));
+  }
+};
+struct F32 {
+  typedef float type;
+};
+
+// Wide accesses at any element: the memory system takes them at the address of an element, and rows of an odd number of
+// 16-bit elements are read like others.
+template <int kBytes>
+struct Wide;
+template <>
+struct Wide<2> {
+  typedef u32x2 two __attribute__((aligned(2)));
+  typedef u32x4 four __attribute__((aligned(2)));
+};
+template <>
+struct Wide<4> {
+  typedef u32x2 two __attribute__((aligned(4)));
+  typedef u32x4 four __attribute__((aligned(4)));
+};
+
+// Eight entries of a row as they lie in memory, in two runs of four.
+template <class Kind>
+struct Piece {
+  typedef typename Kind::type T;
+  static constexpr bool kNarrow = sizeof(T) == 2;
+  uint32_t w[kNarrow ? 4 : 8];
+
+  __device__ __forceinline__ void load_run(int run, const T* p) {
+    if constexpr (kNarrow) {
+      const u32x2 v = *reinterpret_cast<const typename Wide<sizeof(T)>::two*>(p);
+      w[2 * run] = v[0];
+      w[2 * run + 1] = v[1];
+    } else {
+      const u32x4 v = *reinterpret_cast<const typename Wide<sizeof(T)>::four*>(p);
+#pragma unroll
+      for (int x = 0; x < 4; ++x) w[4 * run + x] = v[x];
+    }
+  }
+  __device__ __forceinline__ void load(const T* p) {
+    if constexpr (kNarrow) {
+      const u32x4 v = *reinterpret_cast<const typename Wide<sizeof(T)>::four*>(p);
+#pragma unroll
+      for (int x = 0; x < 4; ++x) w[x] = v[x];
+    } else {
+      load_run(0, p);
+      load_run(1, p + 4);
+    }
+  }
+  __device__ __forceinline__ void set(int e, T x) {
+    if constexpr (kNarrow) {
+      const uint32_t bits = __builtin_bit_cast(uint16_t, x);
+      w[e / 2] = e & 1 ? (w[e / 2] & 0xffffu) | bits << 16 : (w[e / 2] & 0xffff0000u) | bits;
+    } else {
+      w[e] = __float_as_uint(x);
+    }
+  }
+  __device__ __forceinline__ void clear() {
+#pragma unroll
+    for (int x = 0; x < (kNarrow ? 4 : 8); ++x) w[x] = 0;
+  }
+  // The first `count` < 8 of a row's last entries, 0 behind them.
+  __device__ __forceinline__ void load_tail(const T* p, int count) {
+    clear();
+#pragma unroll
+    for (int e = 0; e < kEach - 1; ++e)
+      if (e < count) set(e, p[e]);
+  }
+  __device__ __forceinline__ void unpack(float* x) const {
+#pragma unroll
+    for (int e = 0; e < kEach; e += 2) {
+      f32x2 v;
+      if constexpr (kNarrow)
+        v = Kind::widen(w[e / 2]);
+      else
+        v = f32x2{__uint_as_float(w[e]), __uint_as_float(w[e + 1])};
+      x[e] = v[0];
+      x[e + 1] = v[1];
+    }
+  }
+  __device__ __forceinline__ void pack(const float* x) {
+#pragma unroll
+    for (int e = 0; e < kEach; e += 2) {
+      if constexpr (kNarrow) {
+        w[e / 2] = Kind::narrow(x[e], x[e + 1]);
+      } else {
+        w[e] = __float_as_uint(x[e]);
+        w[e + 1] = __float_as_uint(x[e + 1]);
+      }
+    }
+  }
+  __device__ __forceinline__ void store_run(int run, T* p) const {
+    if constexpr (kNarrow)
+      *reinterpret_cast<typename Wide<sizeof(T)>::two*>(p) = u32x2{w[2 * run], w[2 * run + 1]};
+    else
+      *reinterpret_cast<typename Wide<sizeof(T)>::four*>(p) = u32x4{w[4 * run], w[4 * run + 1], w[4 * run + 2], w[4 * run + 3]};
+  }
+  __device__ __forceinline__ void store(T* p) const {
+    if constexpr (kNarrow) {
+      *reinterpret_cast<typename Wide<sizeof(T)>::four*>(p) = u32x4{w[0], w[1], w[2], w[3]};
+    } else {
+      store_run(0, p);
+      store_run(1, p + 4);
+    }
+  }
+};
+
+__device__ __forceinline__ float load_param(const void* p, int dtype, int64_t at) {
+  if (dtype == LITE_ATTN_F32) return static_cast<const float*>(p)[at];
+  if (dtype == LITE_ATTN_BF16) return (float)static_cast<const __bf16*>(p)[at];
+  return (float)static_cast<const _Float16*>(p)[at];
+}
+
+// ---- sums over a team --------------------------------------------------------------------------------------------------
+
+template <int kCtrl>
+__device__ __forceinline__ float add_dpp(float x) {
+  return x + __uint_as_float(__builtin_amdgcn_update_dpp(0u, __float_as_uint(x), kCtrl, 0xf, 0xf, true));
+}
+__device__ __forceinline__ float add_row_pairs(float x) {  // rows of 16 lanes, 0 with 1 and 2 with 3
+  const u32x2 s = __builtin_amdgcn_permlane16_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+  return __uint_as_float(s[0]) + __uint_as_float(s[1]);
+}
+__device__ __forceinline__ float add_halves(float x) {  // lanes 0..31 with 32..63
+  const u32x2 s = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+  return __uint_as_float(s[0]) + __uint_as_float(s[1]);
+}
+constexpr int kXor1 = 0xB1, kXor2 = 0x4E, kHalfMirror = 0x141, kMirror = 0x140;
+__device__ __forceinline__ float sum16(float x) {
+  return add_dpp<kMirror>(add_dpp<kHalfMirror>(add_dpp<kXor2>(add_dpp<kXor1>(x))));
+}
+__device__ __forceinline__ float sum64(float x) { return add_halves(add_row_pairs(sum16(x))); }
+// Sum over 1 << lanes_log neighbouring lanes, in all of them.
+__device__ __forceinline__ float sum_lanes(float x, int lanes_log) {
+  if (lanes_log >= 1) x = add_dpp<kXor1>(x);
+  if (lanes_log >= 2) x = add_dpp<kXor2>(x);
+  if (lanes_log >= 3) x = add_dpp<kHalfMirror>(x);
+  if (lanes_log >= 4) x = add_dpp<kMirror>(x);
+  if (lanes_log >= 5) x = add_row_pairs(x);
+  if (lanes_log >= 6) x = add_halves(x);
+  return x;
+}
+
+// A barrier that orders LDS alone: loads and stores of global memory stay in flight across it.
+__device__ __forceinline__ void lds_barrier() {
+  __builtin_amdgcn_fence(__ATOMIC_RELEASE, "workgroup", "local");
+  __builtin_amdgcn_s_barrier();
+  __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "workgroup", "local");
+}
+
+// Sums of two values over all waves of the workgroup; `mine` are a wave's own.  The two halves of `room` serve in turn: a wave
+// that is one sum ahead cannot overwrite what another still reads, as there is a barrier between.
+struct WaveRoom {
+  f32x2 v[2][kMaxTeam / 64];
+};
+__device__ __forceinline__ void put_waves(WaveRoom* room, int turn, f32x2 mine) {
+  if ((threadIdx.x & 63) == 0) room->v[turn][threadIdx.x >> 6] = mine;
+}
+__device__ __forceinline__ f32x2 get_waves(const WaveRoom* room, int turn) {
+  const int w = threadIdx.x & 15;
+  f32x2 x = room->v[turn][w];
+  if (w >= (int)(blockDim.x >> 6)) x = f32x2{0.f, 0.f};
+  return x;
+}
+
+// ---- rotary positions --------------------------------------------------------------------------------------------------
+
+// cos and sin of a pair's angle at token n of a batch entry, whose positions are given or null.  In 64 bits until whole turns
+// are off: in 32 an angle of 10^5 radians would be off by 6e-3.
+__device__ __forceinline__ f32x2 angle_of(const RotaryParams& p, const int32_t* positions, int n, int pair) {
+  if (pair >= p.pairs) return f32x2{1.f, 0.f};
+  double p0, p1, p2;
+  if (positions) {
+    p0 = positions[n];
+    p1 = positions[n + (int64_t)p.N];
+    p2 = positions[n + 2 * (int64_t)p.N];
+  } else {
+    int t = p.token_start + n;
+    if (t >= p.video) t = 0;
+    const int f = quotient(t, p.area, p.per_area), in = t - f * p.area;
+    const int y = quotient(in, p.width, p.per_width);
+    p0 = f;
+    p1 = y;
+    p2 = in - y * p.width;
+  }
+  const double* f = p.freqs + pair;
+  double turns = p0 * f[0];
+  turns = __builtin_fma(p1, f[p.pairs], turns);
+  turns = __builtin_fma(p2, f[2 * p.pairs], turns);
+  turns *= 0.15915494309189533577;  // 1 / (2 pi)
+  turns -= __builtin_rint(turns);
+  float s, c;
+  sincospif(2.f * (float)turns, &s, &c);
+  return f32x2{c, s};
+}
+
+// A workgroup: some heads (under NORM_ROW all) of q or k, for a share of consecutive rows, a row being a token.  A thread
+// holds four pairs of a head, a[4] and b[4].
+template <class Kind, bool HALVES, int NORM, bool BWD>
+__global__ __launch_bounds__(NORM == LITE_ATTN_NORM_ROW ? kMaxTeam : 256) void rotary_kernel(const RotaryParams p) {
+  typedef typename Kind::type T;
+  __shared__ f32x2 angles[kAngles];
+  __shared__ WaveRoom room;
+  const int tid = threadIdx.x, threads = blockDim.x;
+  const int parts = p.side[0].groups + p.side[1].groups;
+  const int share = (int)(blockIdx.x / (unsigned)parts), part = (int)(blockIdx.x - share * (unsigned)parts);
+  const int batch = share / p.shares, n0 = share_start(p.N, p.shares, share - batch * p.shares),
+            n1 = share_start(p.N, p.shares, share - batch * p.shares + 1);
+  const int which = part >= p.side[0].groups;
+  const RotarySide& side = p.side[which];
+  const int group = which ? part - p.side[0].groups : part;
+
+  const int lanes = 1 << p.lanes_log;
+  const int slot = tid >> p.lanes_log, c = tid & (lanes - 1);
+  const int head = group * p.team_heads + slot;
+  // entries of the head from this thread's first pair on, in pairs; all four are there but at a head's ragged end
+  const int count = slot < p.team_heads && head < side.heads ? min(4, p.head_dim / 2 - 4 * c) : 0;
+  auto valid = [&](int e) { return e < count; };
+  // places in the head of a[e] and b[e]
+  const int P = p.pairs;
+  auto place_a = [&](int e) {
+    const int i = 4 * c + e;
+    return HALVES && i < P ? i : HALVES ? 2 * P + 2 * (i - P) : 2 * i;
+  };
+  auto place_b = [&](int e) { return HALVES && 4 * c + e < P ? 4 * c + e + P : place_a(e) + 1; };
+  // Whole pieces: eight entries in a row, or, of turned halves, four a and four b.  What else there is -- a head's ragged
+  // end, a piece across the end of the turned halves -- goes entry by entry.
+  const bool apart = HALVES && 4 * c + 4 <= P, whole = count == 4 && (!HALVES || apart || 4 * c >= P);
+  const int first = place_a(0);
+
+  auto fetch = [&](const char* row, int64_t stride_h, Piece<Kind>& to) {
+    const T* at = reinterpret_cast<const T*>(row + head * stride_h);
+    if (whole) {
+      if (HALVES && apart) {
+        to.load_run(0, at + first);
+        to.load_run(1, at + first + P);
+      } else {
+        to.load(at + first);
+      }
+    } else if (count > 0) {
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        if (!valid(e)) continue;
+        to.set(2 * e, at[place_a(e)]);
+        to.set(2 * e + 1, at[place_b(e)]);
+      }
+    }
+  };
+  auto unpack = [&](const Piece<Kind>& from, float* a, float* b) {
+    float x[kEach];
+    from.unpack(x);
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      a[e] = HALVES && apart ? x[e] : x[2 * e];
+      b[e] = HALVES && apart ? x[4 + e] : x[2 * e + 1];
+    }
+  };
+  auto store = [&](char* row, const float* ra, const float* rb) {
+    T* at = reinterpret_cast<T*>(row + head * side.os[1]);
+    float x[kEach];
+#pragma unroll
+    for (int e = 0; e < kEach; ++e) {
+      x[e] = e & 1 ? rb[e / 2] : ra[e / 2];
+      if (HALVES && apart) x[e] = e < 4 ? ra[e & 3] : rb[e & 3];
+    }
+    Piece<Kind> out;
+    if (whole) {
+      out.pack(x);
+      if (HALVES && apart) {
+        out.store_run(0, at + first);
+        out.store_run(1, at + first + P);
+      } else {
+        out.store(at + first);
+      }
+    } else if (count > 0) {
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        if (!valid(e)) continue;
+        at[place_a(e)] = (T)ra[e];
+        at[place_b(e)] = (T)rb[e];
+      }
+    }
+  };
+
+  float wa[4], wb[4], da[4], db[4];  // weights and, backwards, the sums for their gradient
+  if constexpr (NORM != LITE_ATTN_NORM_NONE) {
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      wa[e] = wb[e] = 1.f;
+      da[e] = db[e] = 0.f;
+      if (side.w && valid(e)) {
+        const int row = NORM == LITE_ATTN_NORM_ROW ? head * p.head_dim : 0;
+        wa[e] = load_param(side.w, p.weight_dtype, row + place_a(e));
+        wb[e] = load_param(side.w, p.weight_dtype, row + place_b(e));
+      }
+    }
+  }
+  const char *in_x = side.x + batch * side.xs[0] + n0 * side.xs[2], *in_g = side.g + batch * side.gs[0] + n0 * side.gs[2];
+  char* out = side.out + batch * side.os[0] + n0 * side.os[2];
+  Piece<Kind> next_x, next_g;
+  next_x.clear();
+  next_g.clear();
+  auto fetch_next = [&]() {
+    if (!BWD || NORM != LITE_ATTN_NORM_NONE) {
+      fetch(in_x, side.xs[1], next_x);
+      in_x += side.xs[2];
+    }
+    if (BWD) {
+      fetch(in_g, side.gs[1], next_g);
+      in_g += side.gs[2];
+    }
+  };
+  fetch_next();
+  const int32_t* positions = p.positions ? p.positions + batch * p.positions_stride_b : nullptr;
+  const int pairs_log = p.lanes_log + 2;            // angles of a token, with those of entries that are not turned
+  const int some = max(1, kAngles >> pairs_log);    // tokens whose angles are made at a time
+  int turn = 0;
+  for (int start = n0; start < n1; start += some) {
+    const int stop = min(n1, start + some);
+    if (start != n0) lds_barrier();
+    for (int x = tid; x < (stop - start) << pairs_log; x += threads)
+      angles[x] = angle_of(p, positions, start + (x >> pairs_log), x & ((1 << pairs_log) - 1));
+    lds_barrier();
+    for (int n = start; n < stop; ++n) {
+      const Piece<Kind> x = next_x, g = next_g;
+      if (n + 1 < n1) fetch_next();
+      float ca[4], sa[4];
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        const f32x2 cs = angles[((n - start) << pairs_log) + 4 * c + e];
+        ca[e] = cs[0];
+        sa[e] = cs[1];
+      }
+      float xa[4], xb[4];
+      if constexpr (!BWD) {
+        unpack(x, xa, xb);
+        if constexpr (NORM != LITE_ATTN_NORM_NONE) {
+          float sq = 0.f;
+#pragma unroll
+          for (int e = 0; e < 4; ++e)
+            if (valid(e)) sq += xa[e] * xa[e] + xb[e] * xb[e];
+          if constexpr (NORM == LITE_ATTN_NORM_HEAD) {
+            sq = sum_lanes(sq, p.lanes_log);
+          } else {
+            put_waves(&room, turn, f32x2{sum64(sq), 0.f});
+            lds_barrier();
+            sq = sum16(get_waves(&room, turn)[0]);
+            turn ^= 1;
+          }
+          const float rstd = rsqrtf(sq * side.inv_count + p.eps);
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            xa[e] *= rstd * wa[e];
+            xb[e] *= rstd * wb[e];
+          }
+        }
+        float ra[4], rb[4];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          ra[e] = xa[e] * ca[e] - xb[e] * sa[e];
+          rb[e] = xa[e] * sa[e] + xb[e] * ca[e];
+        }
+        store(out, ra, rb);
+      } else {
+        float ga[4], gb[4], za[4], zb[4];
+        unpack(g, ga, gb);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {  // the turn back
+          za[e] = ga[e] * ca[e] + gb[e] * sa[e];
+          zb[e] = gb[e] * ca[e] - ga[e] * sa[e];
+        }
+        if constexpr (NORM != LITE_ATTN_NORM_NONE) {
+          unpack(x, xa, xb);
+          float sq = 0.f, dot = 0.f;
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            if (!valid(e)) continue;
+            sq += xa[e] * xa[e] + xb[e] * xb[e];
+            dot += za[e] * wa[e] * xa[e] + zb[e] * wb[e] * xb[e];
+          }
+          if constexpr (NORM == LITE_ATTN_NORM_HEAD) {
+            sq = sum_lanes(sq, p.lanes_log);
+            dot = sum_lanes(dot, p.lanes_log);
+          } else {
+            put_waves(&room, turn, f32x2{sum64(sq), sum64(dot)});
+            lds_barrier();
+            const f32x2 all = get_waves(&room, turn);
+            sq = sum16(all[0]);
+            dot = sum16(all[1]);
+            turn ^= 1;
+          }
+          // n = x rstd; dx = rstd (dn - n mean(dn n)), dn = dz w
+          const float rstd = rsqrtf(sq * side.inv_count + p.eps);
+          const float pull = rstd * rstd * (dot * side.inv_count);
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            da[e] += za[e] * (xa[e] * rstd);
+            db[e] += zb[e] * (xb[e] * rstd);
+            za[e] = rstd * (za[e] * wa[e] - xa[e] * pull);
+            zb[e] = rstd * (zb[e] * wb[e] - xb[e] * pull);
+          }
+        }
+        store(out, za, zb);
+      }
+      out += side.os[2];
+    }
+  }
+  if constexpr (BWD && NORM != LITE_ATTN_NORM_NONE) {
+    if (!side.part) return;
+    if constexpr (NORM == LITE_ATTN_NORM_ROW) {
+      float* to = side.part + ((size_t)share * side.heads + head) * p.head_dim;
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        if (!valid(e)) continue;
+        to[place_a(e)] = da[e];
+        to[place_b(e)] = db[e];
+      }
+    } else {  // the heads share their weights: summed in order here, a head's sums after the other's
+      __shared__ float sums[256 * kEach];
+      const int padded = lanes * kEach;
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        sums[tid * kEach + 2 * e] = valid(e) ? da[e] : 0.f;
+        sums[tid * kEach + 2 * e + 1] = valid(e) ? db[e] : 0.f;
+      }
+      lds_barrier();
+      float* to = side.part + ((size_t)share * side.groups + group) * p.head_dim;
+      if (slot == 0) {
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          if (!valid(e)) continue;
+          float ta = 0.f, tb = 0.f;
+          for (int h = 0; h < p.team_heads; ++h) {
+            ta += sums[h * padded + c * kEach + 2 * e];
+            tb += sums[h * padded + c * kEach + 2 * e + 1];
+          }
+          to[place_a(e)] = ta;
+          to[place_b(e)] = tb;
+        }
+      }
+    }
+  }
+}
+
+// out[column] = the sum over `rows` rows of part[row][columns]: a workgroup takes 64 columns, its waves an equal share of the
+// rows each.
+struct RowSums {
+  const float* part[2];
+  float* out[2];
+  int rows[2], columns[2], blocks0;
+};
+__global__ __launch_bounds__(1024) void sum_rows_kernel(const RowSums p) {
+  __shared__ float sums[16][64];
+  const int which = (int)blockIdx.x >= p.blocks0, block = which ? (int)blockIdx.x - p.blocks0 : (int)blockIdx.x;
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const int column = block * 64 + lane, columns = p.columns[which], rows = p.rows[which];
+  const int r1 = share_start(rows, 16, wave + 1);
+  float sum = 0.f;
+  if (column < columns) {
+    const float* from = p.part[which] + column;
+#pragma unroll 8
+    for (int r = share_start(rows, 16, wave); r < r1; ++r) sum += from[(size_t)r * columns];
+  }
+  sums[wave][lane] = sum;
+  __syncthreads();
+  if (wave == 0 && column < columns) {
+    for (int w = 1; w < 16; ++w) sum += sums[w][lane];
+    p.out[which][column] = sum;
+  }
+}
+
+// ---- residual stream ---------------------------------------------------------------------------------------------------
+
+// The columns of a row that a thread holds: from `first` on, all kEach or none or, of RAGGED rows, `count` of them.
+template <bool RAGGED>
+struct Columns {
+  int first, count;
+  __device__ __forceinline__ Columns(int thread, int D) : first(thread * kEach), count(min(kEach, max(0, D - thread * kEach))) {}
+  __device__ __forceinline__ bool has(int e) const { return RAGGED ? e < count : count > 0; }
+  __device__ __forceinline__ bool whole() const { return RAGGED ? count == kEach : count > 0; }
+};
+
+template <class Kind, bool RAGGED>
+__device__ __forceinline__ void load_row(const typename Kind::type* row, const Columns<RAGGED>& col, Piece<Kind>& to) {
+  if (col.whole())
+    to.load(row + col.first);
+  else if constexpr (RAGGED)
+    to.load_tail(row + col.first, col.count);
+}
+template <class Kind, bool RAGGED>
+__device__ __forceinline__ void store_row(typename Kind::type* row, const Columns<RAGGED>& col, const float* x) {
+  if (col.whole()) {
+    Piece<Kind> out;
+    out.pack(x);
+    out.store(row + col.first);
+  } else if constexpr (RAGGED) {
+#pragma unroll
+    for (int e = 0; e < kEach - 1; ++e)
+      if (col.has(e)) row[col.first + e] = (typename Kind::type)x[e];
+  }
+}
+template <class Kind, bool RAGGED>
+__device__ __forceinline__ void load_vector(const void* p, const Columns<RAGGED>& col, float* to) {
+  Piece<Kind> v;
+  v.clear();
+  load_row<Kind>(static_cast<const typename Kind::type*>(p), col, v);
+  v.unpack(to);
+}
+template <bool RAGGED>
+__device__ __forceinline__ void load_params(const void* p, int dtype, const Columns<RAGGED>& col, float* to, float missing) {
+  if (!p) {
+#pragma unroll
+    for (int e = 0; e < kEach; ++e) to[e] = missing;
+  } else if (dtype == LITE_ATTN_F32) {
+    load_vector<F32>(p, col, to);
+  } else if (dtype == LITE_ATTN_BF16) {
+    load_vector<Bf16>(p, col, to);
+  } else {
+    load_vector<F16>(p, col, to);
+  }
+}
+
+// Sums over a row's team: 16 or 32 lanes of a wave, a wave, or all waves of the workgroup.
+struct Team {
+  int log;     // < 6: 1 << log lanes
+  bool waves;  // more than one wave
+  int turn;
+  WaveRoom* room;
+  __device__ __forceinline__ Team(const ResidualParams& p, WaveRoom* room_)
+      : log(p.team_log), waves(p.team > 64), turn(0), room(room_) {}
+  __device__ __forceinline__ float in_wave(float x) const { return log < 6 ? sum_lanes(x, log) : sum64(x); }
+  // This wave's values -> those of wave threadIdx.x % 16 (0 if there is none).
+  __device__ __forceinline__ f32x2 exchange(f32x2 x) {
+    put_waves(room, turn, x);
+    lds_barrier();
+    x = get_waves(room, turn);
+    turn ^= 1;
+    return x;
+  }
+  __device__ __forceinline__ f32x2 sum(f32x2 x) {
+    x = f32x2{in_wave(x[0]), in_wave(x[1])};
+    if (!waves) return x;
+    x = exchange(x);
+    return f32x2{sum16(x[0]), sum16(x[1])};
+  }
+};
+
+// Gradient through a norm: d -> rstd (d - mean(d) [LAYER] - n mean(d n)).
+template <bool RAGGED>
+__device__ __forceinline__ void norm_back(Team& team, float* d, const float* n, float rstd, int kind, float inv_D,
+                                          const Columns<RAGGED>& col) {
+  f32x2 s = {0.f, 0.f};
+#pragma unroll
+  for (int e = 0; e < kEach; ++e) {
+    if (!col.has(e)) continue;
+    s[0] += d[e];
+    s[1] += d[e] * n[e];
+  }
+  s = team.sum(s);
+  const float mean = kind == LITE_ATTN_NORM_LAYER ? s[0] * inv_D : 0.f, pull = s[1] * inv_D;
+#pragma unroll
+  for (int e = 0; e < kEach; ++e) d[e] = rstd * (d[e] - mean - n[e] * pull);
+}
+
+// Mean (0 under RMS) and 1 / standard deviation of a row.  Under LAYER the squares are taken about the wave's own mean, and
+// those of the waves put together (squares about the row's mean = theirs + count * (their mean - the row's)^2): one exchange
+// between waves, and nothing cancels where the mean is large.  `counts`: entries of a row in this wave, and in wave
+// threadIdx.x % 16.
+struct Counts {
+  float mine_inv, other;
+};
+struct Stats {
+  float mean, rstd;
+};
+template <bool RAGGED>
+__device__ __forceinline__ Stats row_stats(Team& team, const float* x, const Columns<RAGGED>& col, int kind, float eps, float inv_D,
+                                           const Counts& counts) {
+  float mean = 0.f;
+  if (kind == LITE_ATTN_NORM_LAYER) {
+    float s = 0.f;
+#pragma unroll
+    for (int e = 0; e < kEach; ++e) s += x[e];  // (0 where the thread has no column)
+    mean = team.in_wave(s) * counts.mine_inv;
+  }
+  float sq = 0.f;
+#pragma unroll
+  for (int e = 0; e < kEach; ++e) {
+    const float d = x[e] - mean;
+    if (col.has(e)) sq += d * d;
+  }
+  sq = team.in_wave(sq);
+  if (team.waves) {
+    f32x2 w = team.exchange(f32x2{mean, sq});
+    if (kind == LITE_ATTN_NORM_LAYER) {
+      mean = sum16(w[0] * counts.other) * inv_D;
+      const float d = w[0] - mean;
+      w[1] += counts.other * d * d;
+    }
+    sq = sum16(w[1]);
+  }
+  return {mean, rsqrtf(sq * inv_D + eps)};
+}
+
+// What a thread of a residual kernel is: its team's share of rows, its columns.  SMALL: several teams in a wave, whose rows are
+// not the same for all of its lanes.
+template <bool SMALL, bool RAGGED>
+struct Place {
+  Columns<RAGGED> col;
+  int share, batch, n0, n1;
+  __device__ __forceinline__ explicit Place(const ResidualParams& p)
+      : col(SMALL ? threadIdx.x & (p.team - 1) : threadIdx.x, p.D),
+        share(SMALL ? (int)((blockIdx.x * blockDim.x + threadIdx.x) >> p.team_log) : (int)blockIdx.x) {
+    batch = share / p.shares;
+    const int part = share - batch * p.shares;
+    n0 = share_start(p.N, p.shares, part);
+    n1 = share_start(p.N, p.shares, part + 1);
+  }
+};
+
+template <bool RAGGED>
+__device__ __forceinline__ Counts count_columns(const ResidualParams& p, const Columns<RAGGED>& col, const Team& team,
+                                                float* in_waves) {
+  if (!team.waves) return {p.inv_D, 0.f};
+  const float mine = sum64((float)col.count);
+  if ((threadIdx.x & 63) == 0) in_waves[threadIdx.x >> 6] = mine;
+  lds_barrier();
+  const int w = threadIdx.x & 15;
+  return {1.f / mine, w < (int)(blockDim.x >> 6) ? in_waves[w] : 0.f};
+}
+
+// A walk over consecutive rows of a tensor, or of none.
+struct Walk {
+  char* at;
+  int64_t stride;
+  __device__ __forceinline__ Walk(const Lines& l, int b, int n) : at(l.data), stride(l.stride_n) {
+    if (at) at += b * l.stride_b + n * stride;
+  }
+  __device__ __forceinline__ explicit operator bool() const { return at != nullptr; }
+  template <class T>
+  __device__ __forceinline__ T* next() {
+    T* const row = reinterpret_cast<T*>(at);
+    at += stride;
+    return row;
+  }
+};
+
+// A row of modulation.
+template <bool RAGGED>
+__device__ __forceinline__ void load_mod(const Lines& l, int dtype, int b, int g, const Columns<RAGGED>& col, float* to,
+                                         float missing) {
+  load_params(l.data ? l.data + b * l.stride_b + g * l.stride_n : nullptr, dtype, col, to, missing);
+}
+
+template <class KindX, class KindY, bool SMALL, bool RAGGED>
+__global__ __launch_bounds__(SMALL ? 256 : kMaxTeam) void residual_fwd_kernel(const ResidualParams p) {
+  typedef typename KindX::type X;
+  typedef typename KindY::type Y;
+  __shared__ WaveRoom room;
+  __shared__ float in_waves[kMaxTeam / 64];
+  const Place<SMALL, RAGGED> place(p);
+  const Columns<RAGGED>& col = place.col;
+  Team team(p, &room);
+  if (place.batch >= p.batch) return;  // (of teams inside a wave only: no barrier is missed)
+  const Counts counts = count_columns(p, col, team, in_waves);
+
+  Walk x_in(p.x, place.batch, place.n0), y_in(p.y, place.batch, place.n0);
+  Walk x_to(p.x_out, place.batch, place.n0), h_to(p.h, place.batch, place.n0);
+  Piece<KindX> next_x;
+  Piece<KindY> next_y;
+  next_x.clear();
+  next_y.clear();
+  auto fetch_next = [&]() {
+    load_row<KindX>(x_in.next<X>(), col, next_x);
+    if (y_in) load_row<KindY>(y_in.next<Y>(), col, next_y);
+  };
+  fetch_next();
+  float open[kEach], mul[kEach], add[kEach];  // x_out = x + open * norm(y);  h = norm(x_out) * mul + add
+  int left = 0;                               // tokens left of the row of modulation
+  for (int n = place.n0; n < place.n1; ++n, --left) {
+    const Piece<KindX> px = next_x;
+    const Piece<KindY> py = next_y;
+    if (n + 1 < place.n1) fetch_next();
+    if (left == 0) {
+      const int g = quotient(n, p.per_mod, p.per_group);
+      left = (g + 1) * p.per_mod - n;
+      float t[kEach];
+      load_mod(p.gate, p.param_dtype, place.batch, g, col, open, 1.f);
+      load_params(p.post_w, p.param_dtype, col, t, 1.f);
+#pragma unroll
+      for (int e = 0; e < kEach; ++e) open[e] *= p.alpha * t[e];
+      load_params(p.pre_w, p.param_dtype, col, mul, 1.f);
+      load_params(p.pre_b, p.param_dtype, col, add, 0.f);
+      load_mod(p.scale, p.param_dtype, place.batch, g, col, t, 0.f);
+#pragma unroll
+      for (int e = 0; e < kEach; ++e) {
+        mul[e] *= 1.f + t[e];
+        add[e] *= 1.f + t[e];
+      }
+      load_mod(p.shift, p.param_dtype, place.batch, g, col, t, 0.f);
+#pragma unroll
+      for (int e = 0; e < kEach; ++e) add[e] += t[e];
+    }
+    float x[kEach];
+    px.unpack(x);
+    if (y_in) {
+      float y[kEach];
+      py.unpack(y);
+      if (p.post != LITE_ATTN_NORM_NONE) {
+        const Stats s = row_stats(team, y, col, p.post, p.post_eps, p.inv_D, counts);
+#pragma unroll
+        for (int e = 0; e < kEach; ++e) y[e] = (y[e] - s.mean) * s.rstd;
+      }
+#pragma unroll
+      for (int e = 0; e < kEach; ++e) x[e] += open[e] * y[e];
+    }
+    if (x_to) store_row<KindX>(x_to.next<X>(), col, x);
+    if (h_to) {
+      if (p.pre != LITE_ATTN_NORM_NONE) {
+        const Stats s = row_stats(team, x, col, p.pre, p.pre_eps, p.inv_D, counts);
+#pragma unroll
+        for (int e = 0; e < kEach; ++e) x[e] = (x[e] - s.mean) * s.rstd;
+      }
+#pragma unroll
+      for (int e = 0; e < kEach; ++e) x[e] = x[e] * mul[e] + add[e];
+      store_row<KindY>(h_to.next<Y>(), col, x);
+    }
+  }
+}
+
+// Backwards, for a row: with n = pre(x), da = dh (1 + scale), dn = da pre_w
+//   dx = dx_out + rstd (dn - mean(dn) [LAYER] - n mean(dn n))
+//   dy = the same of dp post_w, dp = alpha gate dx, with n_y = post(y)
+// and over the tokens of a row of modulation A = sum dh n, S = sum dh, C = sum dx n_y, from which all six gradients of the
+// parameters follow (group_sums_kernel): three sums in registers, where each gradient by itself would need six.
+template <class KindX, class KindY, bool SMALL, bool RAGGED>
+__global__ __launch_bounds__(SMALL ? 256 : kMaxTeam) void residual_bwd_kernel(const ResidualParams p) {
+  typedef typename KindX::type X;
+  typedef typename KindY::type Y;
+  __shared__ WaveRoom room;
+  __shared__ float in_waves[kMaxTeam / 64];
+  const Place<SMALL, RAGGED> place(p);
+  const Columns<RAGGED>& col = place.col;
+  Team team(p, &room);
+  if (place.batch >= p.batch) return;  // (of teams inside a wave only: no barrier is missed)
+  const Counts counts = count_columns(p, col, team, in_waves);
+
+  Walk x_in(p.x, place.batch, place.n0), dh_in(p.dh, place.batch, place.n0);
+  Walk dxo_in(p.dxo, place.batch, place.n0), y_in(p.y, place.batch, place.n0);
+  Walk dx_to(p.dx, place.batch, place.n0), dy_to(p.dy, place.batch, place.n0);
+  Piece<KindX> next_x, dxo;
+  Piece<KindY> next_dh, py;
+  next_x.clear();
+  next_dh.clear();
+  dxo.clear();
+  py.clear();
+  auto fetch_next = [&]() {
+    if (x_in) load_row<KindX>(x_in.next<X>(), col, next_x);
+    if (dh_in) load_row<KindY>(dh_in.next<Y>(), col, next_dh);
+  };
+  fetch_next();
+  float open[kEach], mul[kEach];  // alpha gate post_w, (1 + scale) pre_w
+  float sum_a[kEach], sum_s[kEach], sum_c[kEach];
+#pragma unroll
+  for (int e = 0; e < kEach; ++e) sum_a[e] = sum_s[e] = sum_c[e] = 0.f;
+  int left = 0;  // tokens left of the row of modulation
+  for (int n = place.n0; n < place.n1; ++n) {
+    // what the row needs first is asked for a row ahead, the rest now
+    const Piece<KindX> px = next_x;
+    const Piece<KindY> pdh = next_dh;
+    if (dxo_in) load_row<KindX>(dxo_in.next<X>(), col, dxo);
+    if (y_in) load_row<KindY>(y_in.next<Y>(), col, py);
+    if (n + 1 < place.n1) fetch_next();
+    if (left == 0) {
+      const int g = quotient(n, p.per_mod, p.per_group);
+      left = (g + 1) * p.per_mod - n;
+      float t[kEach];
+      load_mod(p.gate, p.param_dtype, place.batch, g, col, open, 1.f);
+      load_params(p.post_w, p.param_dtype, col, t, 1.f);
+#pragma unroll
+      for (int e = 0; e < kEach; ++e) open[e] *= p.alpha * t[e];
+      load_params(p.pre_w, p.param_dtype, col, mul, 1.f);
+      load_mod(p.scale, p.param_dtype, place.batch, g, col, t, 0.f);
+#pragma unroll
+      for (int e = 0; e < kEach; ++e) mul[e] *= 1.f + t[e];
+    }
+    float dx[kEach];
+    if (dh_in) {
+      float x[kEach];
+      float rstd = 1.f;
+      px.unpack(x);
+      pdh.unpack(dx);
+      if (p.pre != LITE_ATTN_NORM_NONE) {
+        const Stats s = row_stats(team, x, col, p.pre, p.pre_eps, p.inv_D, counts);
+        rstd = s.rstd;
+#pragma unroll
+        for (int e = 0; e < kEach; ++e) x[e] = (x[e] - s.mean) * rstd;
+      }
+#pragma unroll
+      for (int e = 0; e < kEach; ++e) {
+        sum_a[e] += dx[e] * x[e];
+        sum_s[e] += dx[e];
+        dx[e] *= mul[e];
+      }
+      if (p.pre != LITE_ATTN_NORM_NONE) norm_back(team, dx, x, rstd, p.pre, p.inv_D, col);
+    } else {
+#pragma unroll
+      for (int e = 0; e < kEach; ++e) dx[e] = 0.f;
+    }
+    float y[kEach];
+    dxo.unpack(y);
+#pragma unroll
+    for (int e = 0; e < kEach; ++e) dx[e] += y[e];
+    if (dx_to) store_row<KindX>(dx_to.next<X>(), col, dx);
+    float rstd = 1.f;
+    py.unpack(y);
+    if (y_in && p.post != LITE_ATTN_NORM_NONE) {
+      const Stats s = row_stats(team, y, col, p.post, p.post_eps, p.inv_D, counts);
+      rstd = s.rstd;
+#pragma unroll
+      for (int e = 0; e < kEach; ++e) y[e] = (y[e] - s.mean) * rstd;
+    }
+#pragma unroll
+    for (int e = 0; e < kEach; ++e) {
+      sum_c[e] += dx[e] * y[e];
+      dx[e] *= open[e];
+    }
+    if (dy_to) {
+      if (p.post != LITE_ATTN_NORM_NONE) norm_back(team, dx, y, rstd, p.post, p.inv_D, col);
+      store_row<KindY>(dy_to.next<Y>(), col, dx);
+    }
+    // the sums of a share's part of a row of modulation: places grow with the share and with the row of modulation
+    if (--left == 0 || n + 1 == place.n1) {
+      if (p.part) {
+        const int g = quotient(n, p.per_mod, p.per_group);
+        float* to = p.part + ((size_t)place.share + place.batch * (size_t)p.groups + g) * 3 * p.D;
+        store_row<F32>(to, col, sum_a);
+        store_row<F32>(to + p.D, col, sum_s);
+        store_row<F32>(to + 2 * (size_t)p.D, col, sum_c);
+      }
+#pragma unroll
+      for (int e = 0; e < kEach; ++e) sum_a[e] = sum_s[e] = sum_c[e] = 0.f;
+    }
+  }
+}
+
+// Sums of a row of modulation: its shares' sums in order, each of the waves an equal part of them, and what follows from them.
+__global__ __launch_bounds__(1024) void group_sums_kernel(const ResidualParams p, int all_groups) {
+  __shared__ float sums[16][3][64];
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, waves = blockDim.x >> 6;
+  const int column = blockIdx.y * 64 + lane;
+  const size_t D = p.D;
+  for (int group = blockIdx.x; group < all_groups; group += gridDim.x) {
+    const int b = group / p.groups, g = group - b * p.groups;
+    const int64_t end = (int64_t)(g + 1) * p.per_mod;
+    const int s0 = b * p.shares + share_of(p.N, p.shares, g * p.per_mod);
+    const int s1 = b * p.shares + share_of(p.N, p.shares, (int)(end < p.N ? end : p.N) - 1) + 1;
+    const int from = s0 + share_start(s1 - s0, waves, wave), to = s0 + share_start(s1 - s0, waves, wave + 1);
+    float a = 0.f, s = 0.f, c = 0.f;
+    if (column < p.D) {
+      const float* part = p.part + ((size_t)from + group) * 3 * D + column;
+#pragma unroll 4
+      for (int x = from; x < to; ++x, part += 3 * D) {
+        a += part[0];
+        s += part[D];
+        c += part[2 * D];
+      }
+    }
+    sums[wave][0][lane] = a;
+    sums[wave][1][lane] = s;
+    sums[wave][2][lane] = c;
+    __syncthreads();
+    if (wave == 0 && column < p.D) {
+      for (int w = 1; w < waves; ++w) {
+        a += sums[w][0][lane];
+        s += sums[w][1][lane];
+        c += sums[w][2][lane];
+      }
+      const int d = p.param_dtype;
+      const size_t at = (size_t)group * D + column;
+      const float post_w = p.post_w ? load_param(p.post_w, d, column) : 1.f;
+      const float pre_w = p.pre_w ? load_param(p.pre_w, d, column) : 1.f;
+      const float pre_b = p.pre_b ? load_param(p.pre_b, d, column) : 0.f;
+      auto mod = [&](const Lines& l, float missing) {
+        return l.data ? load_param(l.data + b * l.stride_b + g * l.stride_n, d, column) : missing;
+      };
+      const float gate = mod(p.gate, 1.f), open = 1.f + mod(p.scale, 0.f);
+      if (p.dgate) p.dgate[at] = p.alpha * post_w * c;
+      if (p.dscale) p.dscale[at] = pre_w * a + pre_b * s;
+      if (p.dshift) p.dshift[at] = s;
+      if (p.dpre_w || p.dpre_b || p.dpost_w) {
+        float* out = p.group_sums + (size_t)group * 3 * D + column;
+        out[0] = open * a;
+        out[D] = open * s;
+        out[2 * D] = p.alpha * gate * c;
+      }
+    }
+    __syncthreads();
+  }
+}
+
+// Gradients of pre_weight, pre_bias and post_weight: the groups' parts in order.
+__global__ __launch_bounds__(1024) void weight_sums_kernel(const ResidualParams p, int all_groups) {
+  __shared__ float sums[16][64];
+  float* const out = blockIdx.y == 0 ? p.dpre_w : blockIdx.y == 1 ? p.dpre_b : p.dpost_w;
+  if (!out) return;
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const int column = blockIdx.x * 64 + lane;
+  const int from = share_start(all_groups, 16, wave), to = share_start(all_groups, 16, wave + 1);
+  float sum = 0.f;
+  if (column < p.D) {
+    const float* part = p.group_sums + blockIdx.y * (size_t)p.D + column;
+#pragma unroll 8
+    for (int x = from; x < to; ++x) sum += part[(size_t)x * 3 * p.D];
+  }
+  sums[wave][lane] = sum;
+  __syncthreads();
+  if (wave == 0 && column < p.D) {
+    for (int w = 1; w < 16; ++w) sum += sums[w][lane];
+    out[column] = sum;
+  }
+}
+
+template <class Kind, bool HALVES, bool BWD>
+void launch_rotary_norm(const RotaryParams& p, const LayerLaunch& l, hipStream_t st) {
+  if (p.norm == LITE_ATTN_NORM_NONE)
+    rotary_kernel<Kind, HALVES, LITE_ATTN_NORM_NONE, BWD><<<l.blocks, l.threads, 0, st>>>(p);
+  else if (p.norm == LITE_ATTN_NORM_HEAD)
+    rotary_kernel<Kind, HALVES, LITE_ATTN_NORM_HEAD, BWD><<<l.blocks, l.threads, 0, st>>>(p);
+  else
+    rotary_kernel<Kind, HALVES, LITE_ATTN_NORM_ROW, BWD><<<l.blocks, l.threads, 0, st>>>(p);
+}
+template <class Kind>
+void launch_rotary_kind(const RotaryParams& p, const LayerLaunch& l, bool bwd, hipStream_t st) {
+  if (bwd)
+    p.halves ? launch_rotary_norm<Kind, true, true>(p, l, st) : launch_rotary_norm<Kind, false, true>(p, l, st);
+  else
+    p.halves ? launch_rotary_norm<Kind, true, false>(p, l, st) : launch_rotary_norm<Kind, false, false>(p, l, st);
+}
+
+template <class KindX, class KindY, bool SMALL, bool RAGGED>
+void launch_residual_way(const ResidualParams& p, const LayerLaunch& l, bool bwd, hipStream_t st) {
+  if (bwd)
+    residual_bwd_kernel<KindX, KindY, SMALL, RAGGED><<<l.blocks, l.threads, 0, st>>>(p);
+  else
+    residual_fwd_kernel<KindX, KindY, SMALL, RAGGED><<<l.blocks, l.threads, 0, st>>>(p);
+}
+template <class KindX, class KindY>
+void launch_residual_kind(const ResidualParams& p, const LayerLaunch& l, bool bwd, hipStream_t st) {
+  if (p.team_log < 6)
+    launch_residual_way<KindX, KindY, true, false>(p, l, bwd, st);
+  else if (p.D % kEach)
+    launch_residual_way<KindX, KindY, false, true>(p, l, bwd, st);
+  else
+    launch_residual_way<KindX, KindY, false, false>(p, l, bwd, st);
+}
+
+}  // namespace
+
+hipError_t launch_rotary(const RotaryParams& p, const LayerLaunch& l, int dtype, bool bwd, hipStream_t st) {
+  if (dtype == LITE_ATTN_BF16)
+    launch_rotary_kind<Bf16>(p, l, bwd, st);
+  else if (dtype == LITE_ATTN_F16)
+    launch_rotary_kind<F16>(p, l, bwd, st);
+  else
+    launch_rotary_kind<F32>(p, l, bwd, st);
+  return hipGetLastError();
+}
+
+// The shares' sums -> the gradients of the weights of q and k, as far as they are wanted.
+hipError_t launch_rotary_weights(const RotaryParams& p, float* dq_weight, float* dk_weight, hipStream_t st) {
+  RowSums s;
+  float* const out[2] = {dq_weight, dk_weight};
+  int blocks[2];
+  for (int x = 0; x < 2; ++x) {
+    const bool row = p.norm == LITE_ATTN_NORM_ROW;
+    s.part[x] = p.side[x].part;
+    s.out[x] = out[x];
+    s.columns[x] = out[x] ? (row ? p.side[x].heads : 1) * p.head_dim : 0;
+    s.rows[x] = p.N == 0 ? 0 : p.batch * p.shares * (row ? 1 : p.side[x].groups);
+    blocks[x] = (s.columns[x] + 63) / 64;
+  }
+  s.blocks0 = blocks[0];
+  if (blocks[0] + blocks[1] == 0) return hipSuccess;
+  sum_rows_kernel<<<blocks[0] + blocks[1], 1024, 0, st>>>(s);
+  return hipGetLastError();
+}
+
+hipError_t launch_residual(const ResidualParams& p, const LayerLaunch& l, int dtype, int stream_dtype, bool bwd,
+                           hipStream_t st) {
+  if (dtype == LITE_ATTN_F32)
+    launch_residual_kind<F32, F32>(p, l, bwd, st);
+  else if (dtype == LITE_ATTN_BF16 && stream_dtype == LITE_ATTN_BF16)
+    launch_residual_kind<Bf16, Bf16>(p, l, bwd, st);
+  else if (dtype == LITE_ATTN_BF16)
+    launch_residual_kind<F32, Bf16>(p, l, bwd, st);
+  else if (stream_dtype == LITE_ATTN_F16)
+    launch_residual_kind<F16, F16>(p, l, bwd, st);
+  else
+    launch_residual_kind<F32, F16>(p, l, bwd, st);
+  return hipGetLastError();
+}
+
+hipError_t launch_residual_sums(const ResidualParams& p, hipStream_t st) {
+  const int64_t groups = (int64_t)p.batch * p.groups;
+  const unsigned columns = (unsigned)(p.D + 63) / 64;
+  if (groups > 0) {
+    const int64_t shares = p.shares * (int64_t)p.per_mod / p.N + 2;  // of a group, at most
+    const int waves = shares < 32 ? (shares < 8 ? 2 : 4) : 16;
+    const dim3 grid((unsigned)(groups < 65536 ? groups : 65536), columns);
+    group_sums_kernel<<<grid, 64 * waves, 0, st>>>(p, (int)groups);
+    const hipError_t e = hipGetLastError();
+    if (e != hipSuccess) return e;
+  }
+  if (p.dpre_w || p.dpre_b || p.dpost_w) weight_sums_kernel<<<dim3(columns, 3), 1024, 0, st>>>(p, (int)groups);
+  return hipGetLastError();
+}
+
+}  // namespace la
+
+extern "C" {
+
+int lite_attn_rotary_fwd(const lite_attn_rotary_desc_t* desc, const lite_attn_rotary_fwd_t* args, void* hip_stream) {
+  int rc = la::check_rotary(desc);
+  if (rc != LITE_ATTN_OK) return rc;
+  if (!args) return LITE_ATTN_EINVAL;
+  if (desc->seqlen == 0) return LITE_ATTN_OK;
+  la::RotaryParams p;
+  la::LayerLaunch l;
+  rc = la::plan_rotary(*desc, *args, &p, &l);
+  if (rc != LITE_ATTN_OK) return rc;
+  const hipError_t e = la::launch_rotary(p, l, desc->dtype, false, reinterpret_cast<hipStream_t>(hip_stream));
+  return e == hipSuccess ? LITE_ATTN_OK : la::hip_fail(e);
+}
+
+int lite_attn_rotary_bwd(const lite_attn_rotary_desc_t* desc, const lite_attn_rotary_bwd_t* args, void* hip_stream) {
+  int rc = la::check_rotary(desc);
+  if (rc != LITE_ATTN_OK) return rc;
+  if (!args) return LITE_ATTN_EINVAL;
+  la::RotaryParams p;
+  la::LayerLaunch l;
+  rc = la::plan_rotary(*desc, *args, &p, &l);
+  if (rc != LITE_ATTN_OK) return rc;
+  hipStream_t stream = reinterpret_cast<hipStream_t>(hip_stream);
+  hipError_t e = hipSuccess;
+  if (desc->seqlen > 0) e = la::launch_rotary(p, l, desc->dtype, true, stream);
+  if (e == hipSuccess && (args->dq_weight || args->dk_weight))
+    e = la::launch_rotary_weights(p, args->dq_weight, desc->heads_k ? args->dk_weight : nullptr, stream);
+  return e == hipSuccess ? LITE_ATTN_OK : la::hip_fail(e);
+}
+
+int lite_attn_residual_norm_fwd(const lite_attn_residual_desc_t* desc, const lite_attn_residual_fwd_t* args,
+                                void* hip_stream) {
+  int rc = la::check_residual(desc);
+  if (rc != LITE_ATTN_OK) return rc;
+  if (!args) return LITE_ATTN_EINVAL;
+  if (desc->seqlen == 0) return LITE_ATTN_OK;
+  la::ResidualParams p;
+  la::LayerLaunch l;
+  rc = la::plan_residual(*desc, *args, &p, &l);
+  if (rc != LITE_ATTN_OK) return rc;
+  const hipError_t e =
+      la::launch_residual(p, l, desc->dtype, desc->stream_dtype, false, reinterpret_cast<hipStream_t>(hip_stream));
+  return e == hipSuccess ? LITE_ATTN_OK : la::hip_fail(e);
+}
+
+int lite_attn_residual_norm_bwd(const lite_attn_residual_desc_t* desc, const lite_attn_residual_bwd_t* args,
+                                void* hip_stream) {
+  int rc = la::check_residual(desc);
+  if (rc != LITE_ATTN_OK) return rc;
+  if (!args) return LITE_ATTN_EINVAL;
+  la::ResidualParams p;
+  la::LayerLaunch l;
+  rc = la::plan_residual(*desc, *args, &p, &l);
+  if (rc != LITE_ATTN_OK) return rc;
+  hipStream_t stream = reinterpret_cast<hipStream_t>(hip_stream);
+  hipError_t e = hipSuccess;
+  if (desc->seqlen > 0) e = la::launch_residual(p, l, desc->dtype, desc->stream_dtype, true, stream);
+  if (e == hipSuccess && p.part) e = la::launch_residual_sums(p, stream);
+  return e == hipSuccess ? LITE_ATTN_OK : la::hip_fail(e);
+}
+
+}  // extern "C"

@@ -1,0 +1,390 @@
+// Host logic of include/lite_attn_layer.h (no HIP call, no device code): argument checks, and how a call is laid out on the
+// chip.  Also builds with a plain C++ compiler under the CPU sanitizers.
+#include "lite_attn_layer_kernels.h"
+
+#include <algorithm>
+#include <cmath>
+
+#include "lite_attn_kernels.h"
+
+namespace la {
+
+namespace {
+
+constexpr int kCUs = 256;
+constexpr int64_t kMaxRows = (int64_t)1 << 30;  // of a call: row and token numbers stay within quotient()'s range
+
+int size_of(int dtype) { return dtype == LITE_ATTN_F32 ? 4 : 2; }
+bool known(int dtype) { return dtype >= LITE_ATTN_BF16 && dtype <= LITE_ATTN_F32; }
+bool good_eps(float eps) { return eps >= 0.f && std::isfinite(eps); }
+size_t up16(size_t x) { return (x + 15) & ~(size_t)15; }
+
+// A tensor of `n` axes (sizes, strides over them, elements) and a last one of `inner` contiguous elements.
+struct View {
+  const void* data;
+  int n;
+  int64_t size[3], stride[3], inner;
+  int dtype;
+};
+
+View view(const lite_attn_heads_t& t, const lite_attn_rotary_desc_t& d, int heads) {
+  return {t.data, 3, {d.batch, heads, d.seqlen}, {t.stride_b, t.stride_h, t.stride_n}, d.head_dim, d.dtype};
+}
+View view(const lite_attn_rows_t& t, int batch, int rows, int dim, int dtype) {
+  return {t.data, 2, {batch, rows, 0}, {t.stride_b, t.stride_n, 0}, dim, dtype};
+}
+
+// Aligned to its type, strides not negative, its extent within an address; a result has no two elements in one place: each
+// axis steps over all of the axes with smaller strides.
+bool good(const View& v, bool result) {
+  for (int x = 0; x < v.n; ++x)
+    if (v.size[x] == 0) return true;  // nothing there, of which the address need not be one
+  if (!v.data || ((uintptr_t)v.data & (size_of(v.dtype) - 1))) return false;
+  constexpr int64_t kMost = (int64_t)1 << 46;  // elements
+  int64_t extent = v.inner;
+  int order[3] = {0, 1, 2};
+  std::sort(order, order + v.n, [&](int a, int b) { return v.stride[a] < v.stride[b]; });
+  for (int x = 0; x < v.n; ++x) {
+    const int64_t size = v.size[order[x]], stride = v.stride[order[x]];
+    if (size <= 1) continue;
+    if (stride < (result ? extent : 0) || stride > kMost) return false;
+    if (stride > kMost / (size - 1)) return false;
+    extent += stride * (size - 1);
+    if (extent > kMost) return false;
+  }
+  return true;
+}
+
+template <class T>
+bool good_vector(const T* p, int dtype) {
+  return ((uintptr_t)p & (size_of(dtype) - 1)) == 0;
+}
+bool good_grad(const float* p) { return ((uintptr_t)p & 3) == 0; }
+
+// Shares of a batch entry's N rows, for `parts` kinds of workgroups of `waves` waves that run side by side: altogether as many
+// workgroups as the chip holds at `per_simd` waves on each of its SIMDs.
+int shares_of(int batch, int N, int waves, int per_simd, int64_t parts) {
+  const int64_t side_by_side = (int64_t)kCUs * std::max(1, std::min(16, 4 * per_simd / waves));
+  const int64_t each = side_by_side / (parts * batch);
+  return (int)std::max<int64_t>(1, std::min<int64_t>(N, each));
+}
+
+int log2_up(int x) {
+  int l = 0;
+  while ((1 << l) < x) ++l;
+  return l;
+}
+
+struct RotaryShape {
+  int lanes_log, team_heads, threads, shares, groups[2];
+};
+
+RotaryShape rotary_shape(const lite_attn_rotary_desc_t& d, bool bwd) {
+  RotaryShape s;
+  s.lanes_log = log2_up((d.head_dim + kEach - 1) / kEach);
+  const int most = std::max(d.heads_q, d.heads_k), lanes = 1 << s.lanes_log;
+  s.team_heads = d.norm == LITE_ATTN_NORM_ROW ? most : std::min(most, std::max(1, 256 / lanes));
+  s.threads = (s.team_heads * lanes + 63) / 64 * 64;
+  s.groups[0] = (d.heads_q + s.team_heads - 1) / s.team_heads;
+  s.groups[1] = (d.heads_k + s.team_heads - 1) / s.team_heads;
+  s.shares = shares_of(d.batch, d.seqlen, s.threads / 64, bwd ? 4 : 8, s.groups[0] + s.groups[1]);
+  return s;
+}
+
+// Floats that one share leaves for the weights' gradient of a side.
+size_t rotary_part(const lite_attn_rotary_desc_t& d, const RotaryShape& s, int side) {
+  const int heads = side ? d.heads_k : d.heads_q;
+  return (size_t)(d.norm == LITE_ATTN_NORM_ROW ? heads : s.groups[side]) * d.head_dim;
+}
+
+int fill_rotary(const lite_attn_rotary_desc_t& d, const lite_attn_positions_t& at, const void* const weights[2],
+                const RotaryShape& s, RotaryParams* p) {
+  *p = RotaryParams();
+  if (d.pairs > 0 && (!at.freqs || ((uintptr_t)at.freqs & 7))) return LITE_ATTN_EINVAL;
+  if (at.positions) {
+    if (((uintptr_t)at.positions & 3) || at.positions_stride_b < 0 || at.positions_stride_b > ((int64_t)1 << 46))
+      return LITE_ATTN_EINVAL;
+  } else if (at.token_start < 0 || (int64_t)at.token_start + d.seqlen > kMaxRows) {
+    return LITE_ATTN_EINVAL;
+  }
+  for (int x = 0; x < 2; ++x) {
+    if (weights[x] && d.norm == LITE_ATTN_NORM_NONE) return LITE_ATTN_EINVAL;
+    if (!good_vector(weights[x], d.weight_dtype)) return LITE_ATTN_EINVAL;
+    p->side[x].w = weights[x];
+    p->side[x].heads = x ? d.heads_k : d.heads_q;
+    p->side[x].groups = s.groups[x];
+    p->side[x].inv_count = 1.f / (float)(d.head_dim * (d.norm == LITE_ATTN_NORM_ROW ? std::max(1, p->side[x].heads) : 1));
+  }
+  p->freqs = at.freqs;
+  p->positions = at.positions;
+  p->positions_stride_b = at.positions_stride_b;
+  p->batch = d.batch;
+  p->N = d.seqlen;
+  p->shares = s.shares;
+  p->head_dim = d.head_dim;
+  p->pairs = d.pairs;
+  p->lanes_log = s.lanes_log;
+  p->team_heads = s.team_heads;
+  p->norm = d.norm;
+  p->halves = d.halves;
+  p->weight_dtype = d.weight_dtype;
+  p->token_start = at.token_start;
+  p->area = d.grid[1] * d.grid[2];
+  p->width = d.grid[2];
+  p->video = d.grid[0] * p->area;
+  p->eps = d.eps;
+  p->per_area = reciprocal(p->area);
+  p->per_width = reciprocal(p->width);
+  return LITE_ATTN_OK;
+}
+
+void set(int64_t to[3], const lite_attn_heads_t& t, int dtype) {
+  to[0] = t.stride_b * size_of(dtype);
+  to[1] = t.stride_h * size_of(dtype);
+  to[2] = t.stride_n * size_of(dtype);
+}
+Lines lines(const lite_attn_rows_t& t, int dtype) {
+  return {static_cast<char*>(t.data), t.stride_b * size_of(dtype), t.stride_n * size_of(dtype)};
+}
+
+}  // namespace
+
+int check_rotary(const lite_attn_rotary_desc_t* d) {
+  if (!d) return LITE_ATTN_EINVAL;
+  if (d->batch < 1 || d->seqlen < 0 || d->heads_q < 1 || d->heads_k < 0 || d->head_dim < 2 || d->head_dim % 2)
+    return LITE_ATTN_EINVAL;
+  if (!known(d->dtype) || !known(d->weight_dtype)) return LITE_ATTN_EINVAL;
+  if (d->norm != LITE_ATTN_NORM_NONE && d->norm != LITE_ATTN_NORM_HEAD && d->norm != LITE_ATTN_NORM_ROW)
+    return LITE_ATTN_EINVAL;
+  if ((d->halves != 0 && d->halves != 1) || d->pairs < 0 || d->pairs > d->head_dim / 2) return LITE_ATTN_EINVAL;
+  if (d->grid[0] < 1 || d->grid[1] < 1 || d->grid[2] < 1 || !good_eps(d->eps)) return LITE_ATTN_EINVAL;
+  if (d->head_dim > 512) return LITE_ATTN_EUNSUPPORTED;
+  const int64_t lanes = (int64_t)1 << log2_up((d->head_dim + kEach - 1) / kEach), most = std::max(d->heads_q, d->heads_k);
+  if (d->norm == LITE_ATTN_NORM_ROW && most * lanes > kMaxTeam) return LITE_ATTN_EUNSUPPORTED;
+  if (most > 1 << 16) return LITE_ATTN_EUNSUPPORTED;
+  if ((int64_t)d->batch * d->seqlen > kMaxRows) return LITE_ATTN_EUNSUPPORTED;
+  const int64_t area = (int64_t)d->grid[1] * d->grid[2];
+  if (area > kMaxRows || area * d->grid[0] > kMaxRows) return LITE_ATTN_EUNSUPPORTED;
+  return LITE_ATTN_OK;
+}
+
+int plan_rotary(const lite_attn_rotary_desc_t& d, const lite_attn_rotary_fwd_t& a, RotaryParams* p, LayerLaunch* l) {
+  const RotaryShape s = rotary_shape(d, false);
+  const void* const weights[2] = {a.q_weight, a.k_weight};
+  const int rc = fill_rotary(d, a.at, weights, s, p);
+  if (rc != LITE_ATTN_OK) return rc;
+  for (int x = 0; x < (d.heads_k ? 2 : 1); ++x) {
+    const lite_attn_heads_t &in = x ? a.k : a.q, &out = x ? a.k_out : a.q_out;
+    const View vi = view(in, d, p->side[x].heads), vo = view(out, d, p->side[x].heads);
+    if (!good(vi, false) || !good(vo, true)) return LITE_ATTN_EINVAL;
+    p->side[x].x = static_cast<const char*>(in.data);
+    p->side[x].out = static_cast<char*>(out.data);
+    set(p->side[x].xs, in, d.dtype);
+    set(p->side[x].os, out, d.dtype);
+  }
+  l->threads = s.threads;
+  l->blocks = d.batch * s.shares * (s.groups[0] + s.groups[1]);
+  return LITE_ATTN_OK;
+}
+
+int plan_rotary(const lite_attn_rotary_desc_t& d, const lite_attn_rotary_bwd_t& a, RotaryParams* p, LayerLaunch* l) {
+  const RotaryShape s = rotary_shape(d, true);
+  const void* const weights[2] = {a.q_weight, a.k_weight};
+  float* const grads[2] = {a.dq_weight, a.dk_weight};
+  const int rc = fill_rotary(d, a.at, weights, s, p);
+  if (rc != LITE_ATTN_OK) return rc;
+  const bool normed = d.norm != LITE_ATTN_NORM_NONE;
+  if (!normed && (grads[0] || grads[1])) return LITE_ATTN_EINVAL;
+  if (!good_grad(grads[0]) || !good_grad(grads[1])) return LITE_ATTN_EINVAL;
+  if (grads[0] || grads[1]) {
+    if (a.workspace_bytes < lite_attn_rotary_bwd_workspace(&d) || !a.workspace || ((uintptr_t)a.workspace & 15))
+      return LITE_ATTN_EWORKSPACE;
+  }
+  float* part = static_cast<float*>(a.workspace);
+  for (int x = 0; x < (d.heads_k ? 2 : 1); ++x) {
+    const lite_attn_heads_t &in = x ? a.k : a.q, &g = x ? a.dk_out : a.dq_out, &out = x ? a.dk : a.dq;
+    const View vi = view(in, d, p->side[x].heads), vg = view(g, d, p->side[x].heads), vo = view(out, d, p->side[x].heads);
+    if ((normed && !good(vi, false)) || !good(vg, false) || !good(vo, true)) return LITE_ATTN_EINVAL;
+    p->side[x].x = static_cast<const char*>(in.data);
+    p->side[x].g = static_cast<const char*>(g.data);
+    p->side[x].out = static_cast<char*>(out.data);
+    set(p->side[x].xs, in, d.dtype);
+    set(p->side[x].gs, g, d.dtype);
+    set(p->side[x].os, out, d.dtype);
+    if (grads[x]) p->side[x].part = part;
+    part += (size_t)d.batch * s.shares * rotary_part(d, s, x);
+  }
+  l->threads = s.threads;
+  l->blocks = d.batch * s.shares * (s.groups[0] + s.groups[1]);
+  return LITE_ATTN_OK;
+}
+
+namespace {
+
+struct ResidualShape {
+  int team, team_log, threads, shares, blocks;
+};
+
+// A team of threads takes a row of `dim` entries: whole waves or, of short rows that are no ragged ones, 16 or 32 threads,
+// several teams in a workgroup of 256.
+ResidualShape residual_shape(const lite_attn_residual_desc_t& d, bool bwd) {
+  ResidualShape s;
+  const int need = (d.dim + kEach - 1) / kEach;
+  s.team_log = d.dim % kEach || need > 32 ? 6 : need <= 16 ? 4 : 5;
+  s.team = s.team_log < 6 ? 1 << s.team_log : (need + 63) / 64 * 64;
+  s.threads = s.team_log < 6 ? 256 : s.team;
+  const int teams = s.threads / s.team;
+  s.shares = shares_of(d.batch, d.seqlen, std::max(1, s.team / 64), bwd ? 4 : 8, 1);
+  if (teams > 1) s.shares = (int)std::max<int64_t>(1, std::min<int64_t>(d.seqlen, (int64_t)s.shares * (64 >> s.team_log)));
+  s.blocks = (int)(((int64_t)d.batch * s.shares + teams - 1) / teams);
+  return s;
+}
+
+int groups_of(const lite_attn_residual_desc_t& d) {
+  return (int)(((int64_t)d.seqlen + d.tokens_per_mod - 1) / d.tokens_per_mod);
+}
+
+// Rows of modulation, or none.
+bool modulation(const lite_attn_rows_t& t, const lite_attn_residual_desc_t& d, Lines* to) {
+  *to = lines(t, d.param_dtype);
+  return !t.data || good(view(t, d.batch, groups_of(d), d.dim, d.param_dtype), false);
+}
+
+int fill_residual(const lite_attn_residual_desc_t& d, const ResidualShape& s, const lite_attn_rows_t& gate,
+                  const lite_attn_rows_t& scale, const void* post_w, const void* pre_w, const void* pre_b,
+                  ResidualParams* p) {
+  *p = ResidualParams();
+  if (!modulation(gate, d, &p->gate) || !modulation(scale, d, &p->scale)) return LITE_ATTN_EINVAL;
+  for (const void* v : {post_w, pre_w, pre_b})
+    if (!good_vector(v, d.param_dtype)) return LITE_ATTN_EINVAL;
+  p->post_w = post_w;
+  p->pre_w = pre_w;
+  p->pre_b = pre_b;
+  p->batch = d.batch;
+  p->N = d.seqlen;
+  p->D = d.dim;
+  p->per_mod = std::min(d.tokens_per_mod, std::max(1, d.seqlen));
+  p->groups = groups_of(d);
+  p->shares = s.shares;
+  p->team = s.team;
+  p->team_log = s.team_log;
+  p->post = d.post_norm;
+  p->pre = d.pre_norm;
+  p->param_dtype = d.param_dtype;
+  p->post_eps = d.post_eps;
+  p->pre_eps = d.pre_eps;
+  p->alpha = d.residual_scale;
+  p->inv_D = 1.f / (float)d.dim;
+  p->per_group = reciprocal(p->per_mod);
+  return LITE_ATTN_OK;
+}
+
+}  // namespace
+
+int check_residual(const lite_attn_residual_desc_t* d) {
+  if (!d) return LITE_ATTN_EINVAL;
+  if (d->batch < 1 || d->seqlen < 0 || d->dim < 1 || d->tokens_per_mod < 1) return LITE_ATTN_EINVAL;
+  if (!known(d->dtype) || !known(d->stream_dtype) || !known(d->param_dtype)) return LITE_ATTN_EINVAL;
+  for (const int norm : {d->post_norm, d->pre_norm})
+    if (norm != LITE_ATTN_NORM_NONE && norm != LITE_ATTN_NORM_RMS && norm != LITE_ATTN_NORM_LAYER) return LITE_ATTN_EINVAL;
+  if (!good_eps(d->post_eps) || !good_eps(d->pre_eps) || !std::isfinite(d->residual_scale)) return LITE_ATTN_EINVAL;
+  if (d->stream_dtype != d->dtype && d->stream_dtype != LITE_ATTN_F32) return LITE_ATTN_EUNSUPPORTED;
+  if (d->dim > kEach * kMaxTeam) return LITE_ATTN_EUNSUPPORTED;
+  if ((int64_t)d->batch * d->seqlen > kMaxRows) return LITE_ATTN_EUNSUPPORTED;
+  return LITE_ATTN_OK;
+}
+
+int plan_residual(const lite_attn_residual_desc_t& d, const lite_attn_residual_fwd_t& a, ResidualParams* p,
+                  LayerLaunch* l) {
+  const ResidualShape s = residual_shape(d, false);
+  const int rc = fill_residual(d, s, a.gate, a.scale, a.post_weight, a.pre_weight, a.pre_bias, p);
+  if (rc != LITE_ATTN_OK) return rc;
+  if (!modulation(a.shift, d, &p->shift)) return LITE_ATTN_EINVAL;
+  if (!a.x.data || (!a.x_out.data && !a.h.data)) return LITE_ATTN_EINVAL;
+  auto take = [&](const lite_attn_rows_t& t, int dtype, bool result, Lines* to) {
+    *to = lines(t, dtype);
+    return !t.data || good(view(t, d.batch, d.seqlen, d.dim, dtype), result);
+  };
+  if (!take(a.x, d.stream_dtype, false, &p->x) || !take(a.y, d.dtype, false, &p->y) ||
+      !take(a.x_out, d.stream_dtype, true, &p->x_out) || !take(a.h, d.dtype, true, &p->h))
+    return LITE_ATTN_EINVAL;
+  l->threads = s.threads;
+  l->blocks = s.blocks;
+  return LITE_ATTN_OK;
+}
+
+int plan_residual(const lite_attn_residual_desc_t& d, const lite_attn_residual_bwd_t& a, ResidualParams* p,
+                  LayerLaunch* l) {
+  const ResidualShape s = residual_shape(d, true);
+  const int rc = fill_residual(d, s, a.gate, a.scale, a.post_weight, a.pre_weight, a.pre_bias, p);
+  if (rc != LITE_ATTN_OK) return rc;
+  const bool normed_y = d.post_norm != LITE_ATTN_NORM_NONE, normed_x = d.pre_norm != LITE_ATTN_NORM_NONE;
+  if (d.seqlen > 0 && a.dh.data && !a.x_out.data && (normed_x || a.dscale || a.dpre_weight)) return LITE_ATTN_EINVAL;
+  if (d.seqlen > 0 && !a.y.data && ((normed_y && a.dy.data) || a.dgate || a.dpost_weight)) return LITE_ATTN_EINVAL;
+  bool sums = false;
+  for (const float* g : {a.dgate, a.dscale, a.dshift, a.dpost_weight, a.dpre_weight, a.dpre_bias}) {
+    if (!good_grad(g)) return LITE_ATTN_EINVAL;
+    sums = sums || g;
+  }
+  if (!sums && !a.dx.data && !a.dy.data) return LITE_ATTN_EINVAL;
+  if (sums && (!a.workspace || ((uintptr_t)a.workspace & 15) ||
+               a.workspace_bytes < lite_attn_residual_norm_bwd_workspace(&d)))
+    return LITE_ATTN_EWORKSPACE;
+  auto take = [&](const lite_attn_rows_t& t, int dtype, bool result, Lines* to) {
+    *to = lines(t, dtype);
+    return !t.data || good(view(t, d.batch, d.seqlen, d.dim, dtype), result);
+  };
+  if (!take(a.dh, d.dtype, false, &p->dh) || !take(a.dx_out, d.stream_dtype, false, &p->dxo) ||
+      !take(a.x_out, d.stream_dtype, false, &p->x) || !take(a.y, d.dtype, false, &p->y) ||
+      !take(a.dx, d.stream_dtype, true, &p->dx) || !take(a.dy, d.dtype, true, &p->dy))
+    return LITE_ATTN_EINVAL;
+  if (sums) {
+    p->part = static_cast<float*>(a.workspace);
+    p->group_sums = p->part + 3 * (size_t)d.batch * (s.shares + p->groups) * d.dim;
+    p->dgate = a.dgate;
+    p->dscale = a.dscale;
+    p->dshift = a.dshift;
+    p->dpost_w = a.dpost_weight;
+    p->dpre_w = a.dpre_weight;
+    p->dpre_b = a.dpre_bias;
+  }
+  l->threads = s.threads;
+  l->blocks = s.blocks;
+  return LITE_ATTN_OK;
+}
+
+}  // namespace la
+
+extern "C" {
+
+size_t lite_attn_rotary_bwd_workspace(const lite_attn_rotary_desc_t* desc) {
+  if (la::check_rotary(desc) != LITE_ATTN_OK || desc->norm == LITE_ATTN_NORM_NONE) return 0;
+  const la::RotaryShape s = la::rotary_shape(*desc, true);
+  return la::up16(sizeof(float) * desc->batch * s.shares * (la::rotary_part(*desc, s, 0) + la::rotary_part(*desc, s, 1)));
+}
+
+size_t lite_attn_residual_norm_bwd_workspace(const lite_attn_residual_desc_t* desc) {
+  if (la::check_residual(desc) != LITE_ATTN_OK) return 0;
+  const size_t rows = la::residual_shape(*desc, true).shares + 2 * (size_t)la::groups_of(*desc);
+  return la::up16(3 * sizeof(float) * desc->batch * rows * desc->dim);
+}
+
+int lite_attn_rotary_freqs(const int32_t axis_pairs[3], double theta, double* host_freqs) {
+  if (!axis_pairs || !host_freqs || !(theta > 0.0) || !std::isfinite(theta)) return LITE_ATTN_EINVAL;
+  int64_t pairs = 0;
+  for (int a = 0; a < 3; ++a) {
+    if (axis_pairs[a] < 0 || axis_pairs[a] > 256) return LITE_ATTN_EINVAL;
+    pairs += axis_pairs[a];
+  }
+  int64_t at = 0;
+  for (int a = 0; a < 3; ++a) {
+    for (int64_t x = 0; x < pairs; ++x) {
+      const bool mine = x >= at && x < at + axis_pairs[a];
+      host_freqs[a * pairs + x] = mine ? std::pow(theta, -(double)(x - at) / axis_pairs[a]) : 0.0;
+    }
+    at += axis_pairs[a];
+  }
+  return LITE_ATTN_OK;
+}
+
+}  // extern "C"

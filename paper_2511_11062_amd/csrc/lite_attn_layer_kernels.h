@@ -1,0 +1,91 @@
+// Internal interface between the host side of include/lite_attn_layer.h and its kernels (not installed).
+#pragma once
+#include <hip/hip_runtime.h>
+#include <stddef.h>
+#include <stdint.h>
+
+#include "lite_attn_layer.h"
+
+namespace la {
+
+// Both operators go over rows (a token, or some heads of one) with a team of threads that hold kEach entries of the row
+// each, for a whole share of consecutive rows of a batch entry: what depends on the column alone (weights, gate, scale,
+// shift, sums over tokens) stays in registers from row to row.
+constexpr int kEach = 8;
+constexpr int kMaxTeam = 1024;
+constexpr int kAngles = 1024;  // angles of the tokens that a workgroup keeps at a time, 8 bytes each
+
+// One of q and k.
+struct RotarySide {
+  const char* x;      // input (backwards: of the forward pass; null if it is not read)
+  const char* g;      // backwards: gradient of the result
+  char* out;          // result (backwards: gradient of the input)
+  int64_t xs[3], gs[3], os[3];  // strides over batch, heads, tokens, bytes
+  const void* w;      // weights or null
+  float* part;        // backwards: [batch * shares][heads or groups][head_dim] sums for the weights' gradient, or null
+  float inv_count;    // 1 / entries that a norm goes over
+  int heads, groups;  // groups of RotaryParams::team_heads heads
+};
+
+struct RotaryParams {
+  RotarySide side[2];
+  const double* freqs;
+  const int32_t* positions;
+  int64_t positions_stride_b;
+  int batch, N;
+  int shares;            // of consecutive tokens of a batch entry
+  int head_dim, pairs;
+  int lanes_log;         // a head takes 1 << lanes_log threads of kEach entries
+  int team_heads;        // heads that a workgroup takes
+  int norm, halves, weight_dtype;
+  int token_start, area, width, video;  // area = height * width, video = frames * area
+  float eps;
+  uint32_t per_area, per_width;         // reciprocals for quotient()
+};
+
+// Rows of a tensor: the first of the first batch entry, and strides over batch entries and rows, bytes.
+struct Lines {
+  char* data;
+  int64_t stride_b, stride_n;
+};
+
+struct ResidualParams {
+  Lines x, y, x_out, h;   // backwards: x is x_out as stored
+  Lines dh, dxo, dx, dy;
+  Lines gate, scale, shift;
+  const void *post_w, *pre_w, *pre_b;
+  int batch, N, D, per_mod, groups;  // groups of a batch entry
+  int shares;                        // of consecutive rows of a batch entry
+  int team, team_log;                // threads of a row; team_log < 6: several rows in a workgroup
+  int post, pre, param_dtype;
+  float post_eps, pre_eps, alpha, inv_D;
+  float* part;                       // backwards: [batch * (shares + groups)][3][D] sums, or null
+  float *dgate, *dscale, *dshift, *dpost_w, *dpre_w, *dpre_b;
+  float* group_sums;                 // [batch * groups][3][D]: the groups' parts of the weights' gradients
+  uint32_t per_group;                // reciprocal(per_mod)
+};
+
+struct LayerLaunch {
+  int threads, blocks;
+};
+
+// Rows n of a share c of `shares` of N rows: share_start(c) <= n < share_start(c + 1); the share that row n is in.
+constexpr int share_start(int N, int shares, int c) { return (int)((int64_t)N * c / shares); }
+constexpr int share_of(int N, int shares, int n) { return (int)((((int64_t)n + 1) * shares - 1) / N); }
+
+// lite_attn_layer_host.cpp (no HIP calls): checks, and what a call launches
+int check_rotary(const lite_attn_rotary_desc_t* d);
+int plan_rotary(const lite_attn_rotary_desc_t& d, const lite_attn_rotary_fwd_t& a, RotaryParams* p, LayerLaunch* l);
+int plan_rotary(const lite_attn_rotary_desc_t& d, const lite_attn_rotary_bwd_t& a, RotaryParams* p, LayerLaunch* l);
+int check_residual(const lite_attn_residual_desc_t* d);
+int plan_residual(const lite_attn_residual_desc_t& d, const lite_attn_residual_fwd_t& a, ResidualParams* p, LayerLaunch* l);
+int plan_residual(const lite_attn_residual_desc_t& d, const lite_attn_residual_bwd_t& a, ResidualParams* p, LayerLaunch* l);
+
+// lite_attn_layer.hip
+hipError_t launch_rotary(const RotaryParams& p, const LayerLaunch& l, int dtype, bool bwd, hipStream_t st);
+hipError_t launch_rotary_weights(const RotaryParams& p, float* dq_weight, float* dk_weight, hipStream_t st);
+hipError_t launch_residual(const ResidualParams& p, const LayerLaunch& l, int dtype, int stream_dtype, bool bwd,
+                           hipStream_t st);
+hipError_t launch_residual_sums(const ResidualParams& p, hipStream_t st);
+
+}  // namespace la

@@ -1,0 +1,422 @@
+"""Gated residual with the norms around it (lite_attn_residual_norm_fwd / _bwd) against its definition in 64 bits."""
+import pytest
+import torch
+
+import layer_reference as ref
+from paper_2511_11062_amd import layer
+
+pytestmark = pytest.mark.gpu
+
+# What 32-bit arithmetic may add, as a share of the sizes that meet in a result: a mean or a mean of squares is a sum of 8 terms in
+# a thread, 6 steps in a wave, 4 between waves and 4 operations to put the waves' together (22 roundings of 2^-24), a norm needs
+# two of them one after the other, root and factors add 8: below 64 of 2^-24, 2^-18.
+SLACK = 2.0 ** -18
+SCALE = 0.625
+
+
+class Case:
+    def __init__(self, batch=1, n=7, dim=256, per=None, dtype="bf16", stream="f32", params="f32", post="none", pre="layer",
+                 weights=False, mods=True, shift=0, seed=1, offset=0.5):
+        self.__dict__.update(locals())
+        self.per = max(1, n) if per is None else per
+        self.groups = -(-n // self.per)
+        g = self.g = ref.gen(seed)
+
+        def tensor(kind, data=None):
+            flat = torch.full((batch * n * dim + shift,), float("nan"), dtype=ref.TYPES[kind], device="cuda")
+            t = flat[shift:].view(batch, n, dim)
+            if data is not None:
+                t.copy_(data)
+            return t
+
+        self.tensor = tensor
+        size = torch.exp(0.7 * ref.randn(g, dim))
+        self.x = tensor(stream, ref.randn(g, batch, n, dim) * size + offset * ref.randn(g, dim) * size)
+        self.y = tensor(dtype, 1.5 * ref.randn(g, batch, n, dim) + 0.25)
+        mod = (0.3 * ref.randn(g, batch, self.groups, 3, dim)).to(ref.TYPES[params])
+        self.gate, self.scale, self.shift_row = (mod[:, :, i] if mods else None for i in range(3))
+        vec = lambda base, s: (base + s * ref.randn(g, dim)).to(ref.TYPES[params]) if weights else None
+        self.post_w, self.pre_w, self.pre_b = vec(1.0, 0.2), vec(1.0, 0.2), vec(0.0, 0.2)
+        self.desc = layer.make_residual_desc(batch, n, dim, dtype=ref.KINDS[dtype], stream_dtype=ref.KINDS[stream],
+                                             param_dtype=ref.KINDS[params], post_norm=ref.NORMS[post], pre_norm=ref.NORMS[pre],
+                                             residual_scale=SCALE, tokens_per_mod=self.per)
+
+    def arguments(self):
+        return dict(gate=ref.rows_view(self.gate), scale=ref.rows_view(self.scale), post_weight=ref.at(self.post_w),
+                    pre_weight=ref.at(self.pre_w), pre_bias=ref.at(self.pre_b), hip_stream=ref.stream())
+
+    def forward(self, x_out=None, h=None):
+        x_out = self.tensor(self.stream) if x_out is None else x_out
+        h = self.tensor(self.dtype) if h is None else h
+        layer.lite_attn_residual_norm_fwd(self.desc, ref.rows_view(self.x), ref.rows_view(self.y), ref.rows_view(x_out),
+                                          ref.rows_view(h), shift=ref.rows_view(self.shift_row), **self.arguments())
+        return x_out, h
+
+    def mod(self, t, missing, leaf):
+        if t is None:
+            return torch.full((1, 1, self.dim), missing, dtype=torch.float64, device="cuda")
+        return ref.spread(leaf, self.per, self.n)
+
+    def leaves(self):
+        names = ("gate", "scale", "shift_row", "post_w", "pre_w", "pre_b")
+        return {k: getattr(self, k).double().requires_grad_() for k in names if getattr(self, k) is not None}
+
+    def branch(self, y, leaf):
+        p = ref.normed(y, self.post, 1e-6)
+        if "post_w" in leaf:
+            p = p * leaf["post_w"]
+        return SCALE * (ref.spread(leaf["gate"], self.per, self.n) if "gate" in leaf else 1.0) * p
+
+    def block(self, x, leaf):
+        z = ref.normed(x, self.pre, 1e-6)
+        if "pre_w" in leaf:
+            z = z * leaf["pre_w"] + leaf["pre_b"]
+        if "scale" in leaf:
+            z = z * (1.0 + ref.spread(leaf["scale"], self.per, self.n)) + ref.spread(leaf["shift_row"], self.per, self.n)
+        return z
+
+    @staticmethod
+    def rstd(x, kind):
+        if kind == "none":
+            return torch.ones_like(x[..., :1])
+        if kind == "layer":
+            x = x - x.mean(dim=-1, keepdim=True)
+        return 1.0 / torch.sqrt((x * x).mean(dim=-1, keepdim=True) + 1e-6)
+
+    def sizes(self, x, kind):
+        """What meets in an entry of a norm: the entry, the row's mean and, off by a share of themselves, the statistics."""
+        if kind == "none":
+            return x.abs()
+        return self.rstd(x, kind) * (x.abs() + (x.abs().mean(dim=-1, keepdim=True) if kind == "layer" else 0.0))
+
+    def check_forward(self):
+        x_out, h = self.forward()
+        with torch.no_grad():
+            leaf = self.leaves()
+            x, y = self.x.double(), self.y.double()
+            want = x + self.branch(y, leaf)
+            gate = ref.spread(leaf["gate"], self.per, self.n).abs() if "gate" in leaf else 1.0
+            w2 = leaf["post_w"].abs() if "post_w" in leaf else 1.0
+            off = SLACK * (x.abs() + SCALE * gate * w2 * self.sizes(y, self.post))  # of x_out before it is rounded
+            ref.check("x_out", x_out, want, off)
+            # an error of x_out goes through the norm: its own entry's, the row's mean of them, and by way of the deviation
+            # the root of their mean square times the entry
+            r = self.rstd(want, self.pre)
+            n = ref.normed(want, self.pre, 1e-6)
+            through = r * (off + off.mean(dim=-1, keepdim=True) + n.abs() * (off * off).mean(dim=-1, keepdim=True).sqrt())
+            if self.pre == "none":
+                through = off
+            w1 = leaf["pre_w"].abs() if "pre_w" in leaf else 1.0
+            b1 = leaf["pre_b"].abs() if "pre_b" in leaf else 0.0
+            open_ = (1.0 + ref.spread(leaf["scale"], self.per, self.n)).abs() if "scale" in leaf else 1.0
+            sh = ref.spread(leaf["shift_row"], self.per, self.n).abs() if "scale" in leaf else 0.0
+            slack = open_ * w1 * (through + SLACK * self.sizes(want, self.pre)) + SLACK * (open_ * b1 + sh)
+            ref.check("h", h, self.block(want, leaf), slack)
+
+    def gradients(self):
+        dh = self.tensor(self.dtype, ref.randn(self.g, self.batch, self.n, self.dim))
+        dxo = self.tensor(self.stream, ref.randn(self.g, self.batch, self.n, self.dim))
+        return dh, dxo
+
+    def backward(self, dh, dxo, dx=None, dy=None):
+        dx = self.tensor(self.stream) if dx is None else dx
+        dy = self.tensor(self.dtype) if dy is None else dy
+        nan = lambda *s: torch.full(s, float("nan"), device="cuda")
+        rows = lambda t: None if t is None else nan(self.batch, self.groups, self.dim)
+        vec = lambda t: None if t is None else nan(self.dim)
+        d = {"gate": rows(self.gate), "scale": rows(self.scale), "shift_row": rows(self.shift_row), "post_w": vec(self.post_w),
+             "pre_w": vec(self.pre_w), "pre_b": vec(self.pre_b)}
+        need = layer.lite_attn_residual_norm_bwd_workspace(self.desc)
+        space = nan(max(16, need) // 4)
+        layer.lite_attn_residual_norm_bwd(
+            self.desc, ref.rows_view(dh), ref.rows_view(dxo), ref.rows_view(self.x), ref.rows_view(self.y), ref.rows_view(dx),
+            ref.rows_view(dy), dgate=ref.at(d["gate"]), dscale=ref.at(d["scale"]), dshift=ref.at(d["shift_row"]),
+            dpost_weight=ref.at(d["post_w"]), dpre_weight=ref.at(d["pre_w"]), dpre_bias=ref.at(d["pre_b"]),
+            workspace=space.data_ptr(), workspace_bytes=need, **self.arguments())
+        return dx, dy, d
+
+    def check_backward(self):
+        dh, dxo = self.gradients()
+        dx, dy, d = self.backward(dh, dxo)
+        leaf = self.leaves()
+        x, y = self.x.double().requires_grad_(), self.y.double().requires_grad_()
+        front = [k for k in ("scale", "shift_row", "pre_w", "pre_b") if k in leaf]
+        got = torch.autograd.grad(self.block(x, leaf), [x] + [leaf[k] for k in front], dh.double())
+        want = {"x": got[0] + dxo.double(), **dict(zip(front, got[1:]))}
+        back = [k for k in ("gate", "post_w") if k in leaf]
+        got = torch.autograd.grad(self.branch(y, leaf), [y] + [leaf[k] for k in back], want["x"])
+        want.update(y=got[0], **dict(zip(back, got[1:])))
+        with torch.no_grad():
+            one = torch.ones((), dtype=torch.float64, device="cuda")
+            mod = lambda k, f: f(ref.spread(leaf[k], self.per, self.n)).abs() if k in leaf else one
+            vec = lambda k: leaf[k].abs() if k in leaf else one
+            x, y = x.detach(), y.detach()
+
+            def through(dn, v, kind):  # sizes that meet in rstd (dn - mean(dn) - n mean(dn n))
+                if kind == "none":
+                    return dn
+                s = self.sizes(v, kind)
+                return self.rstd(v, kind) * (dn + dn.mean(dim=-1, keepdim=True) + s * (dn * s).mean(dim=-1, keepdim=True))
+
+            dn = dh.double().abs() * mod("scale", lambda t: 1.0 + t) * vec("pre_w")
+            size_x = dxo.double().abs() + 2 * through(dn, x, self.pre)
+            ref.check("dx", dx, want["x"], SLACK * size_x)
+            dp = SCALE * mod("gate", lambda t: t) * vec("post_w")
+            size_y = through(dp * want["x"].abs(), y, self.post) * 2
+            # dx comes with an error of its own, which goes through the norm of y
+            ref.check("dy", dy, want["y"], SLACK * (size_y + through(dp * size_x, y, self.post)))
+            sx, sy = self.sizes(x, self.pre), self.sizes(y, self.post)
+            h = dh.double().abs()
+            open_, gate = mod("scale", lambda t: 1.0 + t), mod("gate", lambda t: t)
+            w1, w2 = vec("pre_w"), vec("post_w")
+            b1 = leaf["pre_b"].abs() if "pre_b" in leaf else 0.0
+            terms = {"shift_row": h, "scale": h * (sx * w1 + b1), "gate": SCALE * size_x * sy * w2, "pre_w": h * open_ * sx,
+                     "pre_b": h * open_, "post_w": SCALE * size_x * sy * gate}
+            for k, t in terms.items():
+                if k not in leaf:
+                    continue
+                if k in ("post_w", "pre_w", "pre_b"):
+                    t = t.expand(self.batch, self.n, self.dim).sum(dim=(0, 1))
+                    count = self.batch * self.n
+                else:
+                    t = t.expand(self.batch, self.n, self.dim)
+                    pad = torch.zeros(self.batch, self.groups * self.per - self.n, self.dim, dtype=t.dtype, device="cuda")
+                    t = torch.cat([t, pad], dim=1).view(self.batch, self.groups, self.per, self.dim).sum(dim=2)
+                    count = self.per
+                # each term is off by a share of its size, their sum by a rounding for each at most
+                ref.check("d" + k, d[k], want[k], t * (2 * SLACK + 2.0 ** -24 * min(count + 8, 4096)))
+
+
+@pytest.mark.parametrize("pre", ["none", "rms", "layer"])
+@pytest.mark.parametrize("post", ["none", "rms", "layer"])
+@pytest.mark.parametrize("dtype,stream,params", [("bf16", "f32", "f32"), ("bf16", "bf16", "bf16"), ("f16", "f16", "f32"),
+                                                 ("f16", "f32", "f16"), ("f32", "f32", "f32")])
+def test_forward_and_backward(dtype, stream, params, post, pre):
+    c = Case(batch=2, n=23, dim=640, per=9, dtype=dtype, stream=stream, params=params, post=post, pre=pre, weights=True)
+    c.check_forward()
+    c.check_backward()
+
+
+# one entry, less than a thread's eight, a wave and a bit, whole waves, the most there may be; odd ones of each
+@pytest.mark.parametrize("dim", [1, 2, 7, 8, 9, 31, 64, 120, 128, 136, 256, 257, 504, 512, 513, 520, 1000, 1111, 1536, 2049, 4097,
+                                 5120, 8191, 8192])
+def test_widths(dim):
+    for pre, post in (("layer", "rms"), ("rms", "layer")):
+        c = Case(batch=2, n=5, dim=dim, per=2, pre=pre, post=post, weights=True, offset=4.0)
+        c.check_forward()
+        c.check_backward()
+
+
+@pytest.mark.parametrize("n,per", [(1, 1), (2, 1), (5, 1), (5, 5), (5, 100), (7, 3), (300, 1), (300, 7), (2500, 2500), (2500, 600),
+                                   (2500, 2499), (9000, 1271)])
+@pytest.mark.parametrize("batch", [1, 3])
+def test_rows_of_modulation(batch, n, per):
+    c = Case(batch=batch, n=n, dim=136, per=per, post="rms", weights=True, dtype="f16", stream="f16")
+    c.check_forward()
+    c.check_backward()
+
+
+def test_many_batch_entries():
+    c = Case(batch=3000, n=2, dim=72, post="layer", weights=True)
+    c.check_forward()
+    c.check_backward()
+
+
+def test_a_mean_far_from_zero():
+    """Rows of a mean a thousand times their deviation: the squares are taken about the mean."""
+    c = Case(n=9, dim=1536, dtype="f32", pre="layer", post="layer", offset=0.0)
+    c.x.copy_(ref.randn(c.g, 1, 9, 1536) + 1000.0)
+    c.y.copy_(ref.randn(c.g, 1, 9, 1536) - 1000.0)
+    c.check_forward()
+    c.check_backward()
+
+
+@pytest.mark.parametrize("shift", [1, 3])
+def test_alignment_and_strides(shift):
+    for dtype, stream in (("bf16", "f32"), ("f16", "f16")):
+        c = Case(batch=2, n=11, dim=264, dtype=dtype, stream=stream, post="rms", weights=True, shift=shift)
+        c.check_forward()
+        c.check_backward()
+    c = Case(batch=2, n=11, dim=264, post="rms")
+    wide = torch.full((11, 2, 300), float("nan"), device="cuda")  # tokens first, rows apart
+    wide[:, :, :264].copy_(c.x.transpose(0, 1))
+    c.x = wide[:, :, :264].transpose(0, 1)
+    c.check_forward()
+    c.check_backward()
+
+
+def test_shared_modulation_and_inputs():
+    """Strides of 0: the gradients come for each batch entry."""
+    c = Case(batch=3, n=6, dim=200, per=4, post="rms")
+    for k in ("gate", "scale", "shift_row"):
+        setattr(c, k, getattr(c, k)[:1].expand(3, -1, -1))
+    c.y = c.y[:1].expand(3, -1, -1)
+    c.check_forward()
+    c.check_backward()
+
+
+def test_what_is_left_out():
+    c = Case(batch=2, n=6, dim=320, mods=False, post="rms")
+    c.check_forward()
+    c.check_backward()
+    # no branch: x_out = x, h its norm
+    c = Case(batch=2, n=6, dim=320, stream="bf16")
+    h, x_out = c.tensor("bf16"), c.tensor("bf16")
+    kw = dict(scale=ref.rows_view(c.scale), shift=ref.rows_view(c.shift_row), hip_stream=ref.stream())
+    layer.lite_attn_residual_norm_fwd(c.desc, ref.rows_view(c.x), None, ref.rows_view(x_out), ref.rows_view(h), **kw)
+    assert torch.equal(x_out, c.x)
+    c.y.zero_()
+    assert torch.equal(h, c.forward()[1])
+    h2 = c.tensor("bf16")
+    layer.lite_attn_residual_norm_fwd(c.desc, ref.rows_view(c.x), None, None, ref.rows_view(h2), **kw)
+    assert torch.equal(h2, h)
+    # no h: the stream alone
+    c = Case(batch=2, n=6, dim=320, post="layer")
+    x_out = c.tensor("f32")
+    layer.lite_attn_residual_norm_fwd(c.desc, ref.rows_view(c.x), ref.rows_view(c.y), ref.rows_view(x_out), None,
+                                      gate=ref.rows_view(c.gate), hip_stream=ref.stream())
+    assert torch.equal(x_out, c.forward()[0])
+
+
+def test_gradients_that_are_left_out():
+    c = Case(batch=2, n=37, dim=320, per=8, post="rms", weights=True)
+    dh, dxo = c.gradients()
+    dx, dy, d = c.backward(dh, dxo)
+    need = layer.lite_attn_residual_norm_bwd_workspace(c.desc)
+    space = torch.empty(need // 4, device="cuda")
+    only = lambda **kw: layer.lite_attn_residual_norm_bwd(
+        c.desc, ref.rows_view(dh), ref.rows_view(dxo), ref.rows_view(c.x), ref.rows_view(c.y), kw.pop("dx", None),
+        kw.pop("dy", None), **dict(c.arguments(), **kw))
+    got = c.tensor("f32")
+    only(dx=ref.rows_view(got))
+    assert torch.equal(got, dx)
+    got = c.tensor("bf16")
+    only(dy=ref.rows_view(got))
+    assert torch.equal(got, dy)
+    for name, key in (("dgate", "gate"), ("dshift", "shift_row"), ("dpre_weight", "pre_w"), ("dpost_weight", "post_w"),
+                      ("dpre_bias", "pre_b"), ("dscale", "scale")):
+        got = torch.full_like(d[key], float("nan"))
+        only(workspace=space.data_ptr(), workspace_bytes=need, **{name: got.data_ptr()})
+        assert torch.equal(got, d[key]), name
+    # no gradient of h: what comes back is dx_out, through the branch; none of x_out: as if it were zero
+    zero = torch.zeros_like(dh)
+    want = c.backward(zero, dxo)
+    dx2, dy2 = c.tensor("f32"), c.tensor("bf16")
+    layer.lite_attn_residual_norm_bwd(c.desc, None, ref.rows_view(dxo), None, ref.rows_view(c.y), ref.rows_view(dx2),
+                                      ref.rows_view(dy2), **c.arguments())
+    assert torch.equal(dx2, dxo) and torch.equal(dy2, want[1])
+    want = c.backward(dh, torch.zeros_like(dxo))
+    layer.lite_attn_residual_norm_bwd(c.desc, ref.rows_view(dh), None, ref.rows_view(c.x), ref.rows_view(c.y),
+                                      ref.rows_view(dx2), ref.rows_view(dy2), **c.arguments())
+    assert torch.equal(dx2, want[0]) and torch.equal(dy2, want[1])
+
+
+def test_in_place():
+    c = Case(batch=2, n=37, dim=520, stream="bf16", post="rms", weights=True)
+    dh, dxo = c.gradients()
+    wdx, wdy, wd = c.backward(dh, dxo)
+    dx, dy, d = c.backward(dh, dxo, dx=dxo, dy=dh)
+    assert torch.equal(dx, wdx) and torch.equal(dy, wdy) and all(torch.equal(d[k], wd[k]) for k in d)
+    want = c.forward()
+    got = c.forward(x_out=c.x, h=c.y)
+    assert torch.equal(got[0], want[0]) and torch.equal(got[1], want[1])
+
+
+def test_no_tokens():
+    c = Case(batch=2, n=0, dim=64, weights=True)
+    c.forward()
+    d = c.backward(*c.gradients())[2]
+    assert all((d[k] == 0).all() for k in ("post_w", "pre_w", "pre_b"))
+
+
+def test_infinities_stay_with_their_token():
+    c = Case(n=9, dim=600, post="rms")
+    clean = [t.clone() for t in c.forward()]
+    c.x[0, 3, 5] = float("inf")
+    c.y[0, 6, 599] = float("nan")
+    others = [0, 1, 2, 4, 5, 7, 8]
+    x_out, h = c.forward()
+    assert torch.equal(x_out[:, others], clean[0][:, others]) and torch.equal(h[:, others], clean[1][:, others])
+    assert torch.isnan(h[0, 3]).any() and torch.isnan(x_out[0, 6]).all() and torch.isnan(h[0, 6]).all()
+    assert torch.isinf(x_out[0, 3, 5])
+
+
+def test_rows_beyond_4_gib():
+    c = Case(n=4, dim=256, dtype="bf16", stream="bf16")
+    want = c.forward()
+    stride = (1 << 30) + 8
+    far = torch.empty(3 * stride + 256, dtype=torch.bfloat16, device="cuda").as_strided((1, 4, 256), (0, stride, 1))
+    far.copy_(c.x)
+    c.x = far
+    got = c.forward(x_out=far)
+    assert torch.equal(got[0], want[0]) and torch.equal(got[1], want[1])
+
+
+def test_gradient_against_differences():
+    """As for any function in 32 bits: the difference quotient's error is that of its two values over the step, and a third
+    derivative's share of the step squared."""
+    c = Case(batch=2, n=5, dim=192, dtype="f32", post="rms", weights=True)
+    dh, dxo = c.gradients()
+    x0, y0 = c.x.clone(), c.y.clone()
+    stored = c.forward()[0]
+    c.x = stored
+    dx, dy, d = c.backward(dh, dxo)
+    c.x = x0.clone()
+    h = 2.0 ** -6
+
+    def f():
+        x_out, out = c.forward()
+        terms = torch.cat([(x_out.double() * dxo.double()).flatten(), (out.double() * dh.double()).flatten()])
+        return terms.sum().item(), terms.abs().sum().item()
+
+    for t0, t, grad in ((x0, c.x, dx), (y0, c.y, dy)):
+        for trial in range(3):
+            v = ref.randn(c.g, *t0.shape)
+            t.copy_(t0 + h * v)
+            up, size = f()
+            t.copy_(t0 - h * v)
+            down, _ = f()
+            t.copy_(t0)
+            want = (grad.double() * v.double()).sum().item()
+            third = h * h * (dh.double().abs() * v.double().abs() ** 3).sum().item() + 1e-3 * abs(want)
+            assert abs((up - down) / (2 * h) - want) <= 2 * SLACK * size / (2 * h) + third
+
+
+def test_same_bits_every_time_on_any_stream_and_from_a_graph():
+    c = Case(batch=2, n=777, dim=1111, per=100, post="rms", weights=True)
+    dh, dxo = c.gradients()
+    want_f, want_b = c.forward(), c.backward(dh, dxo)
+
+    def same(f, b):
+        assert all(torch.equal(x, y) for x, y in zip(f, want_f))
+        assert torch.equal(b[0], want_b[0]) and torch.equal(b[1], want_b[1])
+        assert all(torch.equal(b[2][k], want_b[2][k]) for k in b[2])
+
+    same(c.forward(), c.backward(dh, dxo))
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        f, b = c.forward(), c.backward(dh, dxo)
+    side.synchronize()
+    same(f, b)
+    graph = torch.cuda.CUDAGraph()
+    x_out, h = torch.empty_like(want_f[0]), torch.empty_like(want_f[1])
+    dx, dy = torch.empty_like(want_b[0]), torch.empty_like(want_b[1])
+    d = {k: torch.empty_like(v) for k, v in want_b[2].items()}
+    need = layer.lite_attn_residual_norm_bwd_workspace(c.desc)
+    space = torch.empty(need // 4, device="cuda")
+    torch.cuda.synchronize()
+    with torch.cuda.graph(graph):
+        c.forward(x_out=x_out, h=h)
+        layer.lite_attn_residual_norm_bwd(
+            c.desc, ref.rows_view(dh), ref.rows_view(dxo), ref.rows_view(c.x), ref.rows_view(c.y), ref.rows_view(dx),
+            ref.rows_view(dy), dgate=ref.at(d["gate"]), dscale=ref.at(d["scale"]), dshift=ref.at(d["shift_row"]),
+            dpost_weight=ref.at(d["post_w"]), dpre_weight=ref.at(d["pre_w"]), dpre_bias=ref.at(d["pre_b"]),
+            workspace=space.data_ptr(), workspace_bytes=need, **c.arguments())
+    for _ in range(3):
+        for t in (x_out, h, dx, dy, *d.values()):
+            t.fill_(float("nan"))
+        graph.replay()
+        torch.cuda.synchronize()
+        same((x_out, h), (dx, dy, d))
+        same(c.forward(), c.backward(dh, dxo))
