@@ -54,7 +54,8 @@ typedef struct {
 } lite_attn_rotary_desc_t;
 
 /* One of the tensors [batch, heads, seqlen, head_dim], head_dim contiguous, strides in elements and >= 0: results must not
-   have two elements in one place, inputs may (stride 0).  `data` has the alignment of its type. */
+   have two elements in one place, inputs may (stride 0).  `data` has the alignment of its type.  Heads next to each other in 512 entries (four of 128)
+   lie within 2 GiB (LITE_ATTN_EUNSUPPORTED otherwise). */
 typedef struct {
   void* data;
   int64_t stride_b, stride_h, stride_n;

@@ -46,19 +46,20 @@ struct F32 {
   typedef float type;
 };
 
-// Wide accesses at any element: the memory system takes them at the address of an element, and rows of an odd number of
-// 16-bit elements are read like others.
-template <int kBytes>
-struct Wide;
-template <>
-struct Wide<2> {
-  typedef u32x2 two __attribute__((aligned(2)));
-  typedef u32x4 four __attribute__((aligned(2)));
-};
-template <>
-struct Wide<4> {
-  typedef u32x2 two __attribute__((aligned(4)));
-  typedef u32x4 four __attribute__((aligned(4)));
+// Rows of a tensor, one after the other, read and written through a buffer descriptor: what lies behind the row, or in no row at
+// all, reads as 0 and is not written.  So loads and stores stand in no branch, the compiler counts those in flight, and a wait
+// for a row that was asked for ahead does not wait for the stores behind it.  Offsets need the alignment of an element only.
+typedef __amdgpu_buffer_rsrc_t Buffer;
+constexpr int kBufferFlags = 0x00020000;
+struct Walk {
+  char* at;
+  int64_t stride;
+  int bytes;  // of a row
+  __device__ __forceinline__ Buffer row() const { return __builtin_amdgcn_make_buffer_rsrc(at, 0, bytes, kBufferFlags); }
+  __device__ __forceinline__ Buffer row_if(bool there) const {
+    return __builtin_amdgcn_make_buffer_rsrc(at, 0, there ? bytes : 0, kBufferFlags);
+  }
+  __device__ __forceinline__ void step() { at += stride; }
 };
 
 // Eight entries of a row as they lie in memory, in two runs of four.
@@ -66,47 +67,40 @@ template <class Kind>
 struct Piece {
   typedef typename Kind::type T;
   static constexpr bool kNarrow = sizeof(T) == 2;
+  static constexpr int kSize = sizeof(T);
   uint32_t w[kNarrow ? 4 : 8];
 
-  __device__ __forceinline__ void load_run(int run, const T* p) {
+  __device__ __forceinline__ void load_run(int run, Buffer from, int offset) {
     if constexpr (kNarrow) {
-      const u32x2 v = *reinterpret_cast<const typename Wide<sizeof(T)>::two*>(p);
+      const u32x2 v = __builtin_amdgcn_raw_buffer_load_b64(from, offset, 0, 0);
       w[2 * run] = v[0];
       w[2 * run + 1] = v[1];
     } else {
-      const u32x4 v = *reinterpret_cast<const typename Wide<sizeof(T)>::four*>(p);
+      const u32x4 v = __builtin_amdgcn_raw_buffer_load_b128(from, offset, 0, 0);
 #pragma unroll
       for (int x = 0; x < 4; ++x) w[4 * run + x] = v[x];
     }
   }
-  __device__ __forceinline__ void load(const T* p) {
+  __device__ __forceinline__ void load(Buffer from, int offset) {
     if constexpr (kNarrow) {
-      const u32x4 v = *reinterpret_cast<const typename Wide<sizeof(T)>::four*>(p);
+      const u32x4 v = __builtin_amdgcn_raw_buffer_load_b128(from, offset, 0, 0);
 #pragma unroll
       for (int x = 0; x < 4; ++x) w[x] = v[x];
     } else {
-      load_run(0, p);
-      load_run(1, p + 4);
+      load_run(0, from, offset);
+      load_run(1, from, offset + 16);
     }
   }
-  __device__ __forceinline__ void set(int e, T x) {
+  // Entries e and e + 1, each from a place of its own.
+  __device__ __forceinline__ void load_two(int e, Buffer from, int offset0, int offset1) {
     if constexpr (kNarrow) {
-      const uint32_t bits = __builtin_bit_cast(uint16_t, x);
-      w[e / 2] = e & 1 ? (w[e / 2] & 0xffffu) | bits << 16 : (w[e / 2] & 0xffff0000u) | bits;
+      const uint32_t lo = (uint16_t)__builtin_amdgcn_raw_buffer_load_b16(from, offset0, 0, 0);
+      const uint32_t hi = (uint16_t)__builtin_amdgcn_raw_buffer_load_b16(from, offset1, 0, 0);
+      w[e / 2] = lo | hi << 16;
     } else {
-      w[e] = __float_as_uint(x);
+      w[e] = __builtin_amdgcn_raw_buffer_load_b32(from, offset0, 0, 0);
+      w[e + 1] = __builtin_amdgcn_raw_buffer_load_b32(from, offset1, 0, 0);
     }
-  }
-  __device__ __forceinline__ void clear() {
-#pragma unroll
-    for (int x = 0; x < (kNarrow ? 4 : 8); ++x) w[x] = 0;
-  }
-  // The first `count` < 8 of a row's last entries, 0 behind them.
-  __device__ __forceinline__ void load_tail(const T* p, int count) {
-    clear();
-#pragma unroll
-    for (int e = 0; e < kEach - 1; ++e)
-      if (e < count) set(e, p[e]);
   }
   __device__ __forceinline__ void unpack(float* x) const {
 #pragma unroll
@@ -131,18 +125,27 @@ struct Piece {
       }
     }
   }
-  __device__ __forceinline__ void store_run(int run, T* p) const {
+  __device__ __forceinline__ void store_run(int run, Buffer to, int offset) const {
     if constexpr (kNarrow)
-      *reinterpret_cast<typename Wide<sizeof(T)>::two*>(p) = u32x2{w[2 * run], w[2 * run + 1]};
+      __builtin_amdgcn_raw_buffer_store_b64(u32x2{w[2 * run], w[2 * run + 1]}, to, offset, 0, 0);
     else
-      *reinterpret_cast<typename Wide<sizeof(T)>::four*>(p) = u32x4{w[4 * run], w[4 * run + 1], w[4 * run + 2], w[4 * run + 3]};
+      __builtin_amdgcn_raw_buffer_store_b128(u32x4{w[4 * run], w[4 * run + 1], w[4 * run + 2], w[4 * run + 3]}, to, offset, 0, 0);
   }
-  __device__ __forceinline__ void store(T* p) const {
+  __device__ __forceinline__ void store(Buffer to, int offset) const {
     if constexpr (kNarrow) {
-      *reinterpret_cast<typename Wide<sizeof(T)>::four*>(p) = u32x4{w[0], w[1], w[2], w[3]};
+      __builtin_amdgcn_raw_buffer_store_b128(u32x4{w[0], w[1], w[2], w[3]}, to, offset, 0, 0);
     } else {
-      store_run(0, p);
-      store_run(1, p + 4);
+      store_run(0, to, offset);
+      store_run(1, to, offset + 16);
+    }
+  }
+  __device__ __forceinline__ void store_two(int e, Buffer to, int offset0, int offset1) const {
+    if constexpr (kNarrow) {
+      __builtin_amdgcn_raw_buffer_store_b16((uint16_t)w[e / 2], to, offset0, 0, 0);
+      __builtin_amdgcn_raw_buffer_store_b16((uint16_t)(w[e / 2] >> 16), to, offset1, 0, 0);
+    } else {
+      __builtin_amdgcn_raw_buffer_store_b32(w[e], to, offset0, 0, 0);
+      __builtin_amdgcn_raw_buffer_store_b32(w[e + 1], to, offset1, 0, 0);
     }
   }
 };
@@ -237,10 +240,11 @@ __device__ __forceinline__ f32x2 angle_of(const RotaryParams& p, const int32_t* 
 }
 
 // A workgroup: some heads (under NORM_ROW all) of q or k, for a share of consecutive rows, a row being a token.  A thread
-// holds four pairs of a head, a[4] and b[4].
-template <class Kind, bool HALVES, int NORM, bool BWD>
+// holds four pairs of a head, a[4] and b[4].  WHOLE: they are eight entries in a row or, of turned halves, four and four;
+// otherwise (a head's ragged end, four pairs across the end of the turned halves) every entry is fetched by itself.
+template <class Kind, bool HALVES, bool WHOLE, int NORM, bool BWD>
 __global__ __launch_bounds__(NORM == LITE_ATTN_NORM_ROW ? kMaxTeam : 256) void rotary_kernel(const RotaryParams p) {
-  typedef typename Kind::type T;
+  constexpr int kSize = Piece<Kind>::kSize;
   __shared__ f32x2 angles[kAngles];
   __shared__ WaveRoom room;
   const int tid = threadIdx.x, threads = blockDim.x;
@@ -255,9 +259,9 @@ __global__ __launch_bounds__(NORM == LITE_ATTN_NORM_ROW ? kMaxTeam : 256) void r
   const int lanes = 1 << p.lanes_log;
   const int slot = tid >> p.lanes_log, c = tid & (lanes - 1);
   const int head = group * p.team_heads + slot;
-  // entries of the head from this thread's first pair on, in pairs; all four are there but at a head's ragged end
+  // pairs of the head from this thread's first on
   const int count = slot < p.team_heads && head < side.heads ? min(4, p.head_dim / 2 - 4 * c) : 0;
-  auto valid = [&](int e) { return e < count; };
+  auto valid = [&](int e) { return WHOLE ? count > 0 : e < count; };
   // places in the head of a[e] and b[e]
   const int P = p.pairs;
   auto place_a = [&](int e) {
@@ -265,26 +269,34 @@ __global__ __launch_bounds__(NORM == LITE_ATTN_NORM_ROW ? kMaxTeam : 256) void r
     return HALVES && i < P ? i : HALVES ? 2 * P + 2 * (i - P) : 2 * i;
   };
   auto place_b = [&](int e) { return HALVES && 4 * c + e < P ? 4 * c + e + P : place_a(e) + 1; };
-  // Whole pieces: eight entries in a row, or, of turned halves, four a and four b.  What else there is -- a head's ragged
-  // end, a piece across the end of the turned halves -- goes entry by entry.
-  const bool apart = HALVES && 4 * c + 4 <= P, whole = count == 4 && (!HALVES || apart || 4 * c >= P);
-  const int first = place_a(0);
+  const bool apart = HALVES && 4 * c < P;
+  const int first = place_a(0), second = apart ? first + P : first + 4;
 
-  auto fetch = [&](const char* row, int64_t stride_h, Piece<Kind>& to) {
-    const T* at = reinterpret_cast<const T*>(row + head * stride_h);
-    if (whole) {
-      if (HALVES && apart) {
-        to.load_run(0, at + first);
-        to.load_run(1, at + first + P);
-      } else {
-        to.load(at + first);
-      }
-    } else if (count > 0) {
+  // A wave's rows start at its first head; its other heads are `stride_h` apart.  Entries that are not there lie behind all.
+  const int wave_slot = __builtin_amdgcn_readfirstlane(slot), wave_head = group * p.team_heads + wave_slot;
+  auto walk = [&](const char* data, const int64_t* s) {
+    const int span = (int)(min(63 >> p.lanes_log, side.heads - 1) * s[1]) + p.head_dim * kSize;
+    return Walk{const_cast<char*>(data) + batch * s[0] + n0 * s[2] + wave_head * s[1], s[2], span};
+  };
+  struct Places {
+    int first, second, missing;
+  };
+  auto places = [&](const Walk& w, int64_t stride_h) {
+    const int at = (slot - wave_slot) * (int)stride_h;
+    return count > 0 ? Places{at + first * kSize, at + second * kSize, w.bytes} : Places{w.bytes, w.bytes, w.bytes};
+  };
+  auto fetch = [&](Buffer from, const Places& at, Piece<Kind>& to) {
+    if constexpr (WHOLE && HALVES) {
+      to.load_run(0, from, at.first);
+      to.load_run(1, from, at.second);
+    } else if constexpr (WHOLE) {
+      to.load(from, at.first);
+    } else {
 #pragma unroll
       for (int e = 0; e < 4; ++e) {
-        if (!valid(e)) continue;
-        to.set(2 * e, at[place_a(e)]);
-        to.set(2 * e + 1, at[place_b(e)]);
+        const int a = valid(e) ? at.first + (place_a(e) - first) * kSize : at.missing;
+        const int b = valid(e) ? at.first + (place_b(e) - first) * kSize : at.missing;
+        to.load_two(2 * e, from, a, b);
       }
     }
   };
@@ -293,33 +305,30 @@ __global__ __launch_bounds__(NORM == LITE_ATTN_NORM_ROW ? kMaxTeam : 256) void r
     from.unpack(x);
 #pragma unroll
     for (int e = 0; e < 4; ++e) {
-      a[e] = HALVES && apart ? x[e] : x[2 * e];
-      b[e] = HALVES && apart ? x[4 + e] : x[2 * e + 1];
+      a[e] = WHOLE && HALVES && apart ? x[e] : x[2 * e];
+      b[e] = WHOLE && HALVES && apart ? x[4 + e] : x[2 * e + 1];
     }
   };
-  auto store = [&](char* row, const float* ra, const float* rb) {
-    T* at = reinterpret_cast<T*>(row + head * side.os[1]);
+  auto store = [&](Buffer to, const Places& at, const float* ra, const float* rb) {
     float x[kEach];
 #pragma unroll
     for (int e = 0; e < kEach; ++e) {
       x[e] = e & 1 ? rb[e / 2] : ra[e / 2];
-      if (HALVES && apart) x[e] = e < 4 ? ra[e & 3] : rb[e & 3];
+      if (WHOLE && HALVES && apart) x[e] = e < 4 ? ra[e & 3] : rb[e & 3];
     }
     Piece<Kind> out;
-    if (whole) {
-      out.pack(x);
-      if (HALVES && apart) {
-        out.store_run(0, at + first);
-        out.store_run(1, at + first + P);
-      } else {
-        out.store(at + first);
-      }
-    } else if (count > 0) {
+    out.pack(x);
+    if constexpr (WHOLE && HALVES) {
+      out.store_run(0, to, at.first);
+      out.store_run(1, to, at.second);
+    } else if constexpr (WHOLE) {
+      out.store(to, at.first);
+    } else {
 #pragma unroll
       for (int e = 0; e < 4; ++e) {
-        if (!valid(e)) continue;
-        at[place_a(e)] = (T)ra[e];
-        at[place_b(e)] = (T)rb[e];
+        const int a = valid(e) ? at.first + (place_a(e) - first) * kSize : at.missing;
+        const int b = valid(e) ? at.first + (place_b(e) - first) * kSize : at.missing;
+        out.store_two(2 * e, to, a, b);
       }
     }
   };
@@ -337,22 +346,20 @@ __global__ __launch_bounds__(NORM == LITE_ATTN_NORM_ROW ? kMaxTeam : 256) void r
       }
     }
   }
-  const char *in_x = side.x + batch * side.xs[0] + n0 * side.xs[2], *in_g = side.g + batch * side.gs[0] + n0 * side.gs[2];
-  char* out = side.out + batch * side.os[0] + n0 * side.os[2];
+  Walk in_x = walk(side.x, side.xs), in_g = walk(side.g, side.gs), out = walk(side.out, side.os);
+  const Places at_x = places(in_x, side.xs[1]), at_g = places(in_g, side.gs[1]), at_out = places(out, side.os[1]);
   Piece<Kind> next_x, next_g;
-  next_x.clear();
-  next_g.clear();
-  auto fetch_next = [&]() {
-    if (!BWD || NORM != LITE_ATTN_NORM_NONE) {
-      fetch(in_x, side.xs[1], next_x);
-      in_x += side.xs[2];
+  auto fetch_next = [&](bool there) {
+    if constexpr (!BWD || NORM != LITE_ATTN_NORM_NONE) {
+      fetch(in_x.row_if(there), at_x, next_x);
+      in_x.step();
     }
-    if (BWD) {
-      fetch(in_g, side.gs[1], next_g);
-      in_g += side.gs[2];
+    if constexpr (BWD) {
+      fetch(in_g.row_if(there), at_g, next_g);
+      in_g.step();
     }
   };
-  fetch_next();
+  fetch_next(true);
   const int32_t* positions = p.positions ? p.positions + batch * p.positions_stride_b : nullptr;
   const int pairs_log = p.lanes_log + 2;            // angles of a token, with those of entries that are not turned
   const int some = max(1, kAngles >> pairs_log);    // tokens whose angles are made at a time
@@ -365,7 +372,7 @@ __global__ __launch_bounds__(NORM == LITE_ATTN_NORM_ROW ? kMaxTeam : 256) void r
     lds_barrier();
     for (int n = start; n < stop; ++n) {
       const Piece<Kind> x = next_x, g = next_g;
-      if (n + 1 < n1) fetch_next();
+      fetch_next(n + 1 < n1);
       float ca[4], sa[4];
 #pragma unroll
       for (int e = 0; e < 4; ++e) {
@@ -402,7 +409,7 @@ __global__ __launch_bounds__(NORM == LITE_ATTN_NORM_ROW ? kMaxTeam : 256) void r
           ra[e] = xa[e] * ca[e] - xb[e] * sa[e];
           rb[e] = xa[e] * sa[e] + xb[e] * ca[e];
         }
-        store(out, ra, rb);
+        store(out.row(), at_out, ra, rb);
       } else {
         float ga[4], gb[4], za[4], zb[4];
         unpack(g, ga, gb);
@@ -442,9 +449,9 @@ __global__ __launch_bounds__(NORM == LITE_ATTN_NORM_ROW ? kMaxTeam : 256) void r
             zb[e] = rstd * (zb[e] * wb[e] - xb[e] * pull);
           }
         }
-        store(out, za, zb);
+        store(out.row(), at_out, za, zb);
       }
-      out += side.os[2];
+      out.step();
     }
   }
   if constexpr (BWD && NORM != LITE_ATTN_NORM_NONE) {
@@ -513,39 +520,39 @@ __global__ __launch_bounds__(1024) void sum_rows_kernel(const RowSums p) {
 
 // ---- residual stream ---------------------------------------------------------------------------------------------------
 
-// The columns of a row that a thread holds: from `first` on, all kEach or none or, of RAGGED rows, `count` of them.
+// The columns of a row that a thread holds: kEach in a row, or, of RAGGED rows (of a number of entries that kEach does not
+// divide), one of each `team`.  What lies behind the row reads as 0 and is not written.
 template <bool RAGGED>
 struct Columns {
-  int first, count;
-  __device__ __forceinline__ Columns(int thread, int D) : first(thread * kEach), count(min(kEach, max(0, D - thread * kEach))) {}
-  __device__ __forceinline__ bool has(int e) const { return RAGGED ? e < count : count > 0; }
-  __device__ __forceinline__ bool whole() const { return RAGGED ? count == kEach : count > 0; }
+  int thread, team, D;
+  __device__ __forceinline__ int at(int e) const { return RAGGED ? thread + e * team : thread * kEach + e; }
+  __device__ __forceinline__ bool has(int e) const { return RAGGED ? at(e) < D : thread * kEach < D; }
 };
 
-template <class Kind, bool RAGGED>
-__device__ __forceinline__ void load_row(const typename Kind::type* row, const Columns<RAGGED>& col, Piece<Kind>& to) {
-  if (col.whole())
-    to.load(row + col.first);
-  else if constexpr (RAGGED)
-    to.load_tail(row + col.first, col.count);
-}
-template <class Kind, bool RAGGED>
-__device__ __forceinline__ void store_row(typename Kind::type* row, const Columns<RAGGED>& col, const float* x) {
-  if (col.whole()) {
-    Piece<Kind> out;
-    out.pack(x);
-    out.store(row + col.first);
-  } else if constexpr (RAGGED) {
+template <bool RAGGED, class Kind>
+__device__ __forceinline__ void load_row(Buffer from, const Columns<RAGGED>& col, Piece<Kind>& to) {
+  if constexpr (RAGGED) {
 #pragma unroll
-    for (int e = 0; e < kEach - 1; ++e)
-      if (col.has(e)) row[col.first + e] = (typename Kind::type)x[e];
+    for (int e = 0; e < kEach; e += 2) to.load_two(e, from, col.at(e) * to.kSize, col.at(e + 1) * to.kSize);
+  } else {
+    to.load(from, col.at(0) * to.kSize);
   }
 }
 template <class Kind, bool RAGGED>
-__device__ __forceinline__ void load_vector(const void* p, const Columns<RAGGED>& col, float* to) {
+__device__ __forceinline__ void store_row(Buffer to, const Columns<RAGGED>& col, const float* x) {
+  Piece<Kind> out;
+  out.pack(x);
+  if constexpr (RAGGED) {
+#pragma unroll
+    for (int e = 0; e < kEach; e += 2) out.store_two(e, to, col.at(e) * out.kSize, col.at(e + 1) * out.kSize);
+  } else {
+    out.store(to, col.at(0) * out.kSize);
+  }
+}
+template <class Kind, bool RAGGED>
+__device__ __forceinline__ void load_vector(const char* p, const Columns<RAGGED>& col, float* to) {
   Piece<Kind> v;
-  v.clear();
-  load_row<Kind>(static_cast<const typename Kind::type*>(p), col, v);
+  load_row(Walk{const_cast<char*>(p), 0, col.D * v.kSize}.row(), col, v);
   v.unpack(to);
 }
 template <bool RAGGED>
@@ -554,23 +561,25 @@ __device__ __forceinline__ void load_params(const void* p, int dtype, const Colu
 #pragma unroll
     for (int e = 0; e < kEach; ++e) to[e] = missing;
   } else if (dtype == LITE_ATTN_F32) {
-    load_vector<F32>(p, col, to);
+    load_vector<F32>(static_cast<const char*>(p), col, to);
   } else if (dtype == LITE_ATTN_BF16) {
-    load_vector<Bf16>(p, col, to);
+    load_vector<Bf16>(static_cast<const char*>(p), col, to);
   } else {
-    load_vector<F16>(p, col, to);
+    load_vector<F16>(static_cast<const char*>(p), col, to);
   }
 }
+// A row of modulation.
+template <bool RAGGED>
+__device__ __forceinline__ void load_mod(const Lines& l, int dtype, int b, int g, const Columns<RAGGED>& col, float* to,
+                                         float missing) {
+  load_params(l.data ? l.data + b * l.stride_b + g * l.stride_n : nullptr, dtype, col, to, missing);
+}
 
-// Sums over a row's team: 16 or 32 lanes of a wave, a wave, or all waves of the workgroup.
+// Sums over a row's team, the waves of the workgroup.
 struct Team {
-  int log;     // < 6: 1 << log lanes
-  bool waves;  // more than one wave
+  bool waves;  // more than one
   int turn;
   WaveRoom* room;
-  __device__ __forceinline__ Team(const ResidualParams& p, WaveRoom* room_)
-      : log(p.team_log), waves(p.team > 64), turn(0), room(room_) {}
-  __device__ __forceinline__ float in_wave(float x) const { return log < 6 ? sum_lanes(x, log) : sum64(x); }
   // This wave's values -> those of wave threadIdx.x % 16 (0 if there is none).
   __device__ __forceinline__ f32x2 exchange(f32x2 x) {
     put_waves(room, turn, x);
@@ -580,7 +589,7 @@ struct Team {
     return x;
   }
   __device__ __forceinline__ f32x2 sum(f32x2 x) {
-    x = f32x2{in_wave(x[0]), in_wave(x[1])};
+    x = f32x2{sum64(x[0]), sum64(x[1])};
     if (!waves) return x;
     x = exchange(x);
     return f32x2{sum16(x[0]), sum16(x[1])};
@@ -622,7 +631,7 @@ __device__ __forceinline__ Stats row_stats(Team& team, const float* x, const Col
     float s = 0.f;
 #pragma unroll
     for (int e = 0; e < kEach; ++e) s += x[e];  // (0 where the thread has no column)
-    mean = team.in_wave(s) * counts.mine_inv;
+    mean = sum64(s) * counts.mine_inv;
   }
   float sq = 0.f;
 #pragma unroll
@@ -630,7 +639,7 @@ __device__ __forceinline__ Stats row_stats(Team& team, const float* x, const Col
     const float d = x[e] - mean;
     if (col.has(e)) sq += d * d;
   }
-  sq = team.in_wave(sq);
+  sq = sum64(sq);
   if (team.waves) {
     f32x2 w = team.exchange(f32x2{mean, sq});
     if (kind == LITE_ATTN_NORM_LAYER) {
@@ -643,108 +652,82 @@ __device__ __forceinline__ Stats row_stats(Team& team, const float* x, const Col
   return {mean, rsqrtf(sq * inv_D + eps)};
 }
 
-// What a thread of a residual kernel is: its team's share of rows, its columns.  SMALL: several teams in a wave, whose rows are
-// not the same for all of its lanes.
-template <bool SMALL, bool RAGGED>
-struct Place {
-  Columns<RAGGED> col;
-  int share, batch, n0, n1;
-  __device__ __forceinline__ explicit Place(const ResidualParams& p)
-      : col(SMALL ? threadIdx.x & (p.team - 1) : threadIdx.x, p.D),
-        share(SMALL ? (int)((blockIdx.x * blockDim.x + threadIdx.x) >> p.team_log) : (int)blockIdx.x) {
-    batch = share / p.shares;
-    const int part = share - batch * p.shares;
+// The workgroup's share of rows.
+struct Share {
+  int batch, n0, n1;
+  __device__ __forceinline__ explicit Share(const ResidualParams& p) {
+    batch = (int)blockIdx.x / p.shares;
+    const int part = (int)blockIdx.x - batch * p.shares;
     n0 = share_start(p.N, p.shares, part);
     n1 = share_start(p.N, p.shares, part + 1);
+  }
+  __device__ __forceinline__ Walk walk(const Lines& l, int bytes) const {
+    return Walk{l.data + batch * l.stride_b + n0 * l.stride_n, l.stride_n, l.data ? bytes : 0};
   }
 };
 
 template <bool RAGGED>
-__device__ __forceinline__ Counts count_columns(const ResidualParams& p, const Columns<RAGGED>& col, const Team& team,
-                                                float* in_waves) {
-  if (!team.waves) return {p.inv_D, 0.f};
-  const float mine = sum64((float)col.count);
+__device__ __forceinline__ Counts count_columns(const ResidualParams& p, const Columns<RAGGED>& col, float* in_waves) {
+  float mine = 0.f;
+#pragma unroll
+  for (int e = 0; e < kEach; ++e) mine += col.has(e) ? 1.f : 0.f;
+  mine = sum64(mine);
   if ((threadIdx.x & 63) == 0) in_waves[threadIdx.x >> 6] = mine;
   lds_barrier();
   const int w = threadIdx.x & 15;
   return {1.f / mine, w < (int)(blockDim.x >> 6) ? in_waves[w] : 0.f};
 }
 
-// A walk over consecutive rows of a tensor, or of none.
-struct Walk {
-  char* at;
-  int64_t stride;
-  __device__ __forceinline__ Walk(const Lines& l, int b, int n) : at(l.data), stride(l.stride_n) {
-    if (at) at += b * l.stride_b + n * stride;
-  }
-  __device__ __forceinline__ explicit operator bool() const { return at != nullptr; }
-  template <class T>
-  __device__ __forceinline__ T* next() {
-    T* const row = reinterpret_cast<T*>(at);
-    at += stride;
-    return row;
-  }
-};
-
-// A row of modulation.
-template <bool RAGGED>
-__device__ __forceinline__ void load_mod(const Lines& l, int dtype, int b, int g, const Columns<RAGGED>& col, float* to,
-                                         float missing) {
-  load_params(l.data ? l.data + b * l.stride_b + g * l.stride_n : nullptr, dtype, col, to, missing);
-}
-
-template <class KindX, class KindY, bool SMALL, bool RAGGED>
-__global__ __launch_bounds__(SMALL ? 256 : kMaxTeam) void residual_fwd_kernel(const ResidualParams p) {
-  typedef typename KindX::type X;
-  typedef typename KindY::type Y;
+template <class KindX, class KindY, bool RAGGED>
+__global__ __launch_bounds__(kMaxTeam) void residual_fwd_kernel(const ResidualParams p) {
   __shared__ WaveRoom room;
   __shared__ float in_waves[kMaxTeam / 64];
-  const Place<SMALL, RAGGED> place(p);
-  const Columns<RAGGED>& col = place.col;
-  Team team(p, &room);
-  if (place.batch >= p.batch) return;  // (of teams inside a wave only: no barrier is missed)
-  const Counts counts = count_columns(p, col, team, in_waves);
+  const Share share(p);
+  const Columns<RAGGED> col = {(int)threadIdx.x, (int)blockDim.x, p.D};
+  Team team = {blockDim.x > 64, 0, &room};
+  const int row_x = p.D * Piece<KindX>::kSize, row_y = p.D * Piece<KindY>::kSize;
 
-  Walk x_in(p.x, place.batch, place.n0), y_in(p.y, place.batch, place.n0);
-  Walk x_to(p.x_out, place.batch, place.n0), h_to(p.h, place.batch, place.n0);
+  Walk x_in = share.walk(p.x, row_x), y_in = share.walk(p.y, row_y);
+  Walk x_to = share.walk(p.x_out, row_x), h_to = share.walk(p.h, row_y);
   Piece<KindX> next_x;
   Piece<KindY> next_y;
-  next_x.clear();
-  next_y.clear();
-  auto fetch_next = [&]() {
-    load_row<KindX>(x_in.next<X>(), col, next_x);
-    if (y_in) load_row<KindY>(y_in.next<Y>(), col, next_y);
+  auto fetch_next = [&](bool there) {
+    load_row(x_in.row_if(there), col, next_x);
+    load_row(y_in.row_if(there), col, next_y);
+    x_in.step();
+    y_in.step();
   };
-  fetch_next();
+  fetch_next(true);
+  const Counts counts = count_columns(p, col, in_waves);
   float open[kEach], mul[kEach], add[kEach];  // x_out = x + open * norm(y);  h = norm(x_out) * mul + add
   int left = 0;                               // tokens left of the row of modulation
-  for (int n = place.n0; n < place.n1; ++n, --left) {
+  for (int n = share.n0; n < share.n1; ++n, --left) {
     const Piece<KindX> px = next_x;
     const Piece<KindY> py = next_y;
-    if (n + 1 < place.n1) fetch_next();
+    fetch_next(n + 1 < share.n1);
     if (left == 0) {
       const int g = quotient(n, p.per_mod, p.per_group);
       left = (g + 1) * p.per_mod - n;
       float t[kEach];
-      load_mod(p.gate, p.param_dtype, place.batch, g, col, open, 1.f);
+      load_mod(p.gate, p.param_dtype, share.batch, g, col, open, 1.f);
       load_params(p.post_w, p.param_dtype, col, t, 1.f);
 #pragma unroll
       for (int e = 0; e < kEach; ++e) open[e] *= p.alpha * t[e];
       load_params(p.pre_w, p.param_dtype, col, mul, 1.f);
       load_params(p.pre_b, p.param_dtype, col, add, 0.f);
-      load_mod(p.scale, p.param_dtype, place.batch, g, col, t, 0.f);
+      load_mod(p.scale, p.param_dtype, share.batch, g, col, t, 0.f);
 #pragma unroll
       for (int e = 0; e < kEach; ++e) {
         mul[e] *= 1.f + t[e];
         add[e] *= 1.f + t[e];
       }
-      load_mod(p.shift, p.param_dtype, place.batch, g, col, t, 0.f);
+      load_mod(p.shift, p.param_dtype, share.batch, g, col, t, 0.f);
 #pragma unroll
       for (int e = 0; e < kEach; ++e) add[e] += t[e];
     }
     float x[kEach];
     px.unpack(x);
-    if (y_in) {
+    if (p.y.data) {
       float y[kEach];
       py.unpack(y);
       if (p.post != LITE_ATTN_NORM_NONE) {
@@ -755,8 +738,9 @@ __global__ __launch_bounds__(SMALL ? 256 : kMaxTeam) void residual_fwd_kernel(co
 #pragma unroll
       for (int e = 0; e < kEach; ++e) x[e] += open[e] * y[e];
     }
-    if (x_to) store_row<KindX>(x_to.next<X>(), col, x);
-    if (h_to) {
+    store_row<KindX>(x_to.row(), col, x);
+    x_to.step();
+    if (p.h.data) {
       if (p.pre != LITE_ATTN_NORM_NONE) {
         const Stats s = row_stats(team, x, col, p.pre, p.pre_eps, p.inv_D, counts);
 #pragma unroll
@@ -764,8 +748,9 @@ __global__ __launch_bounds__(SMALL ? 256 : kMaxTeam) void residual_fwd_kernel(co
       }
 #pragma unroll
       for (int e = 0; e < kEach; ++e) x[e] = x[e] * mul[e] + add[e];
-      store_row<KindY>(h_to.next<Y>(), col, x);
     }
+    store_row<KindY>(h_to.row(), col, x);
+    h_to.step();
   }
 }
 
@@ -774,59 +759,57 @@ __global__ __launch_bounds__(SMALL ? 256 : kMaxTeam) void residual_fwd_kernel(co
 //   dy = the same of dp post_w, dp = alpha gate dx, with n_y = post(y)
 // and over the tokens of a row of modulation A = sum dh n, S = sum dh, C = sum dx n_y, from which all six gradients of the
 // parameters follow (group_sums_kernel): three sums in registers, where each gradient by itself would need six.
-template <class KindX, class KindY, bool SMALL, bool RAGGED>
-__global__ __launch_bounds__(SMALL ? 256 : kMaxTeam) void residual_bwd_kernel(const ResidualParams p) {
-  typedef typename KindX::type X;
-  typedef typename KindY::type Y;
+template <class KindX, class KindY, bool RAGGED>
+__global__ __launch_bounds__(kMaxTeam) void residual_bwd_kernel(const ResidualParams p) {
   __shared__ WaveRoom room;
   __shared__ float in_waves[kMaxTeam / 64];
-  const Place<SMALL, RAGGED> place(p);
-  const Columns<RAGGED>& col = place.col;
-  Team team(p, &room);
-  if (place.batch >= p.batch) return;  // (of teams inside a wave only: no barrier is missed)
-  const Counts counts = count_columns(p, col, team, in_waves);
+  const Share share(p);
+  const Columns<RAGGED> col = {(int)threadIdx.x, (int)blockDim.x, p.D};
+  Team team = {blockDim.x > 64, 0, &room};
+  const int row_x = p.D * Piece<KindX>::kSize, row_y = p.D * Piece<KindY>::kSize;
 
-  Walk x_in(p.x, place.batch, place.n0), dh_in(p.dh, place.batch, place.n0);
-  Walk dxo_in(p.dxo, place.batch, place.n0), y_in(p.y, place.batch, place.n0);
-  Walk dx_to(p.dx, place.batch, place.n0), dy_to(p.dy, place.batch, place.n0);
+  Walk x_in = share.walk(p.x, row_x), dh_in = share.walk(p.dh, row_y);
+  Walk dxo_in = share.walk(p.dxo, row_x), y_in = share.walk(p.y, row_y);
+  Walk dx_to = share.walk(p.dx, row_x), dy_to = share.walk(p.dy, row_y);
   Piece<KindX> next_x, dxo;
   Piece<KindY> next_dh, py;
-  next_x.clear();
-  next_dh.clear();
-  dxo.clear();
-  py.clear();
-  auto fetch_next = [&]() {
-    if (x_in) load_row<KindX>(x_in.next<X>(), col, next_x);
-    if (dh_in) load_row<KindY>(dh_in.next<Y>(), col, next_dh);
+  auto fetch_next = [&](bool there) {
+    load_row(x_in.row_if(there), col, next_x);
+    load_row(dh_in.row_if(there), col, next_dh);
+    x_in.step();
+    dh_in.step();
   };
-  fetch_next();
+  fetch_next(true);
+  const Counts counts = count_columns(p, col, in_waves);
   float open[kEach], mul[kEach];  // alpha gate post_w, (1 + scale) pre_w
   float sum_a[kEach], sum_s[kEach], sum_c[kEach];
 #pragma unroll
   for (int e = 0; e < kEach; ++e) sum_a[e] = sum_s[e] = sum_c[e] = 0.f;
   int left = 0;  // tokens left of the row of modulation
-  for (int n = place.n0; n < place.n1; ++n) {
+  for (int n = share.n0; n < share.n1; ++n) {
     // what the row needs first is asked for a row ahead, the rest now
     const Piece<KindX> px = next_x;
     const Piece<KindY> pdh = next_dh;
-    if (dxo_in) load_row<KindX>(dxo_in.next<X>(), col, dxo);
-    if (y_in) load_row<KindY>(y_in.next<Y>(), col, py);
-    if (n + 1 < place.n1) fetch_next();
+    load_row(dxo_in.row(), col, dxo);
+    load_row(y_in.row(), col, py);
+    dxo_in.step();
+    y_in.step();
+    fetch_next(n + 1 < share.n1);
     if (left == 0) {
       const int g = quotient(n, p.per_mod, p.per_group);
       left = (g + 1) * p.per_mod - n;
       float t[kEach];
-      load_mod(p.gate, p.param_dtype, place.batch, g, col, open, 1.f);
+      load_mod(p.gate, p.param_dtype, share.batch, g, col, open, 1.f);
       load_params(p.post_w, p.param_dtype, col, t, 1.f);
 #pragma unroll
       for (int e = 0; e < kEach; ++e) open[e] *= p.alpha * t[e];
       load_params(p.pre_w, p.param_dtype, col, mul, 1.f);
-      load_mod(p.scale, p.param_dtype, place.batch, g, col, t, 0.f);
+      load_mod(p.scale, p.param_dtype, share.batch, g, col, t, 0.f);
 #pragma unroll
       for (int e = 0; e < kEach; ++e) mul[e] *= 1.f + t[e];
     }
     float dx[kEach];
-    if (dh_in) {
+    if (p.dh.data) {
       float x[kEach];
       float rstd = 1.f;
       px.unpack(x);
@@ -852,10 +835,11 @@ __global__ __launch_bounds__(SMALL ? 256 : kMaxTeam) void residual_bwd_kernel(co
     dxo.unpack(y);
 #pragma unroll
     for (int e = 0; e < kEach; ++e) dx[e] += y[e];
-    if (dx_to) store_row<KindX>(dx_to.next<X>(), col, dx);
+    store_row<KindX>(dx_to.row(), col, dx);
+    dx_to.step();
     float rstd = 1.f;
     py.unpack(y);
-    if (y_in && p.post != LITE_ATTN_NORM_NONE) {
+    if (p.y.data && p.post != LITE_ATTN_NORM_NONE) {
       const Stats s = row_stats(team, y, col, p.post, p.post_eps, p.inv_D, counts);
       rstd = s.rstd;
 #pragma unroll
@@ -866,18 +850,21 @@ __global__ __launch_bounds__(SMALL ? 256 : kMaxTeam) void residual_bwd_kernel(co
       sum_c[e] += dx[e] * y[e];
       dx[e] *= open[e];
     }
-    if (dy_to) {
-      if (p.post != LITE_ATTN_NORM_NONE) norm_back(team, dx, y, rstd, p.post, p.inv_D, col);
-      store_row<KindY>(dy_to.next<Y>(), col, dx);
-    }
+    if (p.dy.data && p.post != LITE_ATTN_NORM_NONE) norm_back(team, dx, y, rstd, p.post, p.inv_D, col);
+    store_row<KindY>(dy_to.row(), col, dx);
+    dy_to.step();
     // the sums of a share's part of a row of modulation: places grow with the share and with the row of modulation
-    if (--left == 0 || n + 1 == place.n1) {
+    if (--left == 0 || n + 1 == share.n1) {
       if (p.part) {
         const int g = quotient(n, p.per_mod, p.per_group);
-        float* to = p.part + ((size_t)place.share + place.batch * (size_t)p.groups + g) * 3 * p.D;
-        store_row<F32>(to, col, sum_a);
-        store_row<F32>(to + p.D, col, sum_s);
-        store_row<F32>(to + 2 * (size_t)p.D, col, sum_c);
+        const int64_t bytes = 4 * (int64_t)p.D;
+        char* to = reinterpret_cast<char*>(p.part) + 3 * bytes * ((int64_t)blockIdx.x + share.batch * (int64_t)p.groups + g);
+        Walk sums = {to, bytes, (int)bytes};
+        store_row<F32>(sums.row(), col, sum_a);
+        sums.step();
+        store_row<F32>(sums.row(), col, sum_s);
+        sums.step();
+        store_row<F32>(sums.row(), col, sum_c);
       }
 #pragma unroll
       for (int e = 0; e < kEach; ++e) sum_a[e] = sum_s[e] = sum_c[e] = 0.f;
@@ -962,38 +949,38 @@ __global__ __launch_bounds__(1024) void weight_sums_kernel(const ResidualParams 
   }
 }
 
-template <class Kind, bool HALVES, bool BWD>
+template <class Kind, bool HALVES, bool WHOLE, bool BWD>
 void launch_rotary_norm(const RotaryParams& p, const LayerLaunch& l, hipStream_t st) {
   if (p.norm == LITE_ATTN_NORM_NONE)
-    rotary_kernel<Kind, HALVES, LITE_ATTN_NORM_NONE, BWD><<<l.blocks, l.threads, 0, st>>>(p);
+    rotary_kernel<Kind, HALVES, WHOLE, LITE_ATTN_NORM_NONE, BWD><<<l.blocks, l.threads, 0, st>>>(p);
   else if (p.norm == LITE_ATTN_NORM_HEAD)
-    rotary_kernel<Kind, HALVES, LITE_ATTN_NORM_HEAD, BWD><<<l.blocks, l.threads, 0, st>>>(p);
+    rotary_kernel<Kind, HALVES, WHOLE, LITE_ATTN_NORM_HEAD, BWD><<<l.blocks, l.threads, 0, st>>>(p);
   else
-    rotary_kernel<Kind, HALVES, LITE_ATTN_NORM_ROW, BWD><<<l.blocks, l.threads, 0, st>>>(p);
+    rotary_kernel<Kind, HALVES, WHOLE, LITE_ATTN_NORM_ROW, BWD><<<l.blocks, l.threads, 0, st>>>(p);
+}
+template <class Kind, bool BWD>
+void launch_rotary_way(const RotaryParams& p, const LayerLaunch& l, hipStream_t st) {
+  const bool whole = p.head_dim % kEach == 0 && (!p.halves || p.pairs % 4 == 0);
+  if (p.halves)
+    whole ? launch_rotary_norm<Kind, true, true, BWD>(p, l, st) : launch_rotary_norm<Kind, true, false, BWD>(p, l, st);
+  else
+    whole ? launch_rotary_norm<Kind, false, true, BWD>(p, l, st) : launch_rotary_norm<Kind, false, false, BWD>(p, l, st);
 }
 template <class Kind>
 void launch_rotary_kind(const RotaryParams& p, const LayerLaunch& l, bool bwd, hipStream_t st) {
-  if (bwd)
-    p.halves ? launch_rotary_norm<Kind, true, true>(p, l, st) : launch_rotary_norm<Kind, false, true>(p, l, st);
-  else
-    p.halves ? launch_rotary_norm<Kind, true, false>(p, l, st) : launch_rotary_norm<Kind, false, false>(p, l, st);
+  bwd ? launch_rotary_way<Kind, true>(p, l, st) : launch_rotary_way<Kind, false>(p, l, st);
 }
 
-template <class KindX, class KindY, bool SMALL, bool RAGGED>
+template <class KindX, class KindY, bool RAGGED>
 void launch_residual_way(const ResidualParams& p, const LayerLaunch& l, bool bwd, hipStream_t st) {
   if (bwd)
-    residual_bwd_kernel<KindX, KindY, SMALL, RAGGED><<<l.blocks, l.threads, 0, st>>>(p);
+    residual_bwd_kernel<KindX, KindY, RAGGED><<<l.blocks, l.threads, 0, st>>>(p);
   else
-    residual_fwd_kernel<KindX, KindY, SMALL, RAGGED><<<l.blocks, l.threads, 0, st>>>(p);
+    residual_fwd_kernel<KindX, KindY, RAGGED><<<l.blocks, l.threads, 0, st>>>(p);
 }
 template <class KindX, class KindY>
 void launch_residual_kind(const ResidualParams& p, const LayerLaunch& l, bool bwd, hipStream_t st) {
-  if (p.team_log < 6)
-    launch_residual_way<KindX, KindY, true, false>(p, l, bwd, st);
-  else if (p.D % kEach)
-    launch_residual_way<KindX, KindY, false, true>(p, l, bwd, st);
-  else
-    launch_residual_way<KindX, KindY, false, false>(p, l, bwd, st);
+  p.D % kEach ? launch_residual_way<KindX, KindY, true>(p, l, bwd, st) : launch_residual_way<KindX, KindY, false>(p, l, bwd, st);
 }
 
 }  // namespace

@@ -149,6 +149,12 @@ Lines lines(const lite_attn_rows_t& t, int dtype) {
 
 }  // namespace
 
+// A wave's heads (512 entries, of ragged heads fewer) lie within 2 GiB of each other: their offsets have 31 bits.
+static bool near(const lite_attn_heads_t& t, const lite_attn_rotary_desc_t& d, int heads) {
+  const int in_wave = std::min(heads, std::max(1, 64 >> log2_up((d.head_dim + kEach - 1) / kEach)));
+  return in_wave == 1 || t.stride_h <= (((int64_t)1 << 31) - 4096) / size_of(d.dtype) / (in_wave - 1);
+}
+
 int check_rotary(const lite_attn_rotary_desc_t* d) {
   if (!d) return LITE_ATTN_EINVAL;
   if (d->batch < 1 || d->seqlen < 0 || d->heads_q < 1 || d->heads_k < 0 || d->head_dim < 2 || d->head_dim % 2)
@@ -177,6 +183,7 @@ int plan_rotary(const lite_attn_rotary_desc_t& d, const lite_attn_rotary_fwd_t& 
     const lite_attn_heads_t &in = x ? a.k : a.q, &out = x ? a.k_out : a.q_out;
     const View vi = view(in, d, p->side[x].heads), vo = view(out, d, p->side[x].heads);
     if (!good(vi, false) || !good(vo, true)) return LITE_ATTN_EINVAL;
+    if (!near(in, d, p->side[x].heads) || !near(out, d, p->side[x].heads)) return LITE_ATTN_EUNSUPPORTED;
     p->side[x].x = static_cast<const char*>(in.data);
     p->side[x].out = static_cast<char*>(out.data);
     set(p->side[x].xs, in, d.dtype);
@@ -205,6 +212,8 @@ int plan_rotary(const lite_attn_rotary_desc_t& d, const lite_attn_rotary_bwd_t& 
     const lite_attn_heads_t &in = x ? a.k : a.q, &g = x ? a.dk_out : a.dq_out, &out = x ? a.dk : a.dq;
     const View vi = view(in, d, p->side[x].heads), vg = view(g, d, p->side[x].heads), vo = view(out, d, p->side[x].heads);
     if ((normed && !good(vi, false)) || !good(vg, false) || !good(vo, true)) return LITE_ATTN_EINVAL;
+    if ((normed && !near(in, d, p->side[x].heads)) || !near(g, d, p->side[x].heads) || !near(out, d, p->side[x].heads))
+      return LITE_ATTN_EUNSUPPORTED;
     p->side[x].x = static_cast<const char*>(in.data);
     p->side[x].g = static_cast<const char*>(g.data);
     p->side[x].out = static_cast<char*>(out.data);
@@ -222,21 +231,14 @@ int plan_rotary(const lite_attn_rotary_desc_t& d, const lite_attn_rotary_bwd_t& 
 namespace {
 
 struct ResidualShape {
-  int team, team_log, threads, shares, blocks;
+  int threads, shares;
 };
 
-// A team of threads takes a row of `dim` entries: whole waves or, of short rows that are no ragged ones, 16 or 32 threads,
-// several teams in a workgroup of 256.
+// A workgroup takes a row of `dim` entries, kEach in a thread.
 ResidualShape residual_shape(const lite_attn_residual_desc_t& d, bool bwd) {
   ResidualShape s;
-  const int need = (d.dim + kEach - 1) / kEach;
-  s.team_log = d.dim % kEach || need > 32 ? 6 : need <= 16 ? 4 : 5;
-  s.team = s.team_log < 6 ? 1 << s.team_log : (need + 63) / 64 * 64;
-  s.threads = s.team_log < 6 ? 256 : s.team;
-  const int teams = s.threads / s.team;
-  s.shares = shares_of(d.batch, d.seqlen, std::max(1, s.team / 64), bwd ? 4 : 8, 1);
-  if (teams > 1) s.shares = (int)std::max<int64_t>(1, std::min<int64_t>(d.seqlen, (int64_t)s.shares * (64 >> s.team_log)));
-  s.blocks = (int)(((int64_t)d.batch * s.shares + teams - 1) / teams);
+  s.threads = (d.dim + 64 * kEach - 1) / (64 * kEach) * 64;
+  s.shares = shares_of(d.batch, d.seqlen, s.threads / 64, bwd ? 4 : 8, 1);
   return s;
 }
 
@@ -266,8 +268,6 @@ int fill_residual(const lite_attn_residual_desc_t& d, const ResidualShape& s, co
   p->per_mod = std::min(d.tokens_per_mod, std::max(1, d.seqlen));
   p->groups = groups_of(d);
   p->shares = s.shares;
-  p->team = s.team;
-  p->team_log = s.team_log;
   p->post = d.post_norm;
   p->pre = d.pre_norm;
   p->param_dtype = d.param_dtype;
@@ -309,7 +309,7 @@ int plan_residual(const lite_attn_residual_desc_t& d, const lite_attn_residual_f
       !take(a.x_out, d.stream_dtype, true, &p->x_out) || !take(a.h, d.dtype, true, &p->h))
     return LITE_ATTN_EINVAL;
   l->threads = s.threads;
-  l->blocks = s.blocks;
+  l->blocks = d.batch * s.shares;
   return LITE_ATTN_OK;
 }
 
@@ -349,7 +349,7 @@ int plan_residual(const lite_attn_residual_desc_t& d, const lite_attn_residual_b
     p->dpre_b = a.dpre_bias;
   }
   l->threads = s.threads;
-  l->blocks = s.blocks;
+  l->blocks = d.batch * s.shares;
   return LITE_ATTN_OK;
 }
 

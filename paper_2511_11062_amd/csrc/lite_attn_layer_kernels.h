@@ -56,7 +56,6 @@ struct ResidualParams {
   const void *post_w, *pre_w, *pre_b;
   int batch, N, D, per_mod, groups;  // groups of a batch entry
   int shares;                        // of consecutive rows of a batch entry
-  int team, team_log;                // threads of a row; team_log < 6: several rows in a workgroup
   int post, pre, param_dtype;
   float post_eps, pre_eps, alpha, inv_D;
   float* part;                       // backwards: [batch * (shares + groups)][3][D] sums, or null
