@@ -62,6 +62,15 @@ struct Walk {
   __device__ __forceinline__ void step() { at += stride; }
 };
 
+// Stores that are dropped.  Before a loop that asks for a row ahead, as many as a row has behind that: the compiler counts what
+// is in flight at the loop's head by the way with the least, and would otherwise wait for a row's stores where it waits for the
+// next row.
+template <int kCount>
+__device__ __forceinline__ void no_stores(const Walk& to) {
+#pragma unroll
+  for (int x = 0; x < kCount; ++x) __builtin_amdgcn_raw_buffer_store_b32(0u, to.row_if(false), 0, 0, 0);
+}
+
 // Eight entries of a row as they lie in memory, in two runs of four.
 template <class Kind>
 struct Piece {
@@ -250,8 +259,7 @@ __global__ __launch_bounds__(NORM == LITE_ATTN_NORM_ROW ? kMaxTeam : 256) void r
   const int tid = threadIdx.x, threads = blockDim.x;
   const int parts = p.side[0].groups + p.side[1].groups;
   const int share = (int)(blockIdx.x / (unsigned)parts), part = (int)(blockIdx.x - share * (unsigned)parts);
-  const int batch = share / p.shares, n0 = share_start(p.N, p.shares, share - batch * p.shares),
-            n1 = share_start(p.N, p.shares, share - batch * p.shares + 1);
+  const int batch = share / p.shares, n0 = share - batch * p.shares, step = p.shares;
   const int which = part >= p.side[0].groups;
   const RotarySide& side = p.side[which];
   const int group = which ? part - p.side[0].groups : part;
@@ -276,7 +284,7 @@ __global__ __launch_bounds__(NORM == LITE_ATTN_NORM_ROW ? kMaxTeam : 256) void r
   const int wave_slot = __builtin_amdgcn_readfirstlane(slot), wave_head = group * p.team_heads + wave_slot;
   auto walk = [&](const char* data, const int64_t* s) {
     const int span = (int)(min(63 >> p.lanes_log, side.heads - 1) * s[1]) + p.head_dim * kSize;
-    return Walk{const_cast<char*>(data) + batch * s[0] + n0 * s[2] + wave_head * s[1], s[2], span};
+    return Walk{const_cast<char*>(data) + batch * s[0] + n0 * s[2] + wave_head * s[1], step * s[2], span};
   };
   struct Places {
     int first, second, missing;
@@ -361,98 +369,99 @@ __global__ __launch_bounds__(NORM == LITE_ATTN_NORM_ROW ? kMaxTeam : 256) void r
   };
   fetch_next(true);
   const int32_t* positions = p.positions ? p.positions + batch * p.positions_stride_b : nullptr;
-  const int pairs_log = p.lanes_log + 2;            // angles of a token, with those of entries that are not turned
-  const int some = max(1, kAngles >> pairs_log);    // tokens whose angles are made at a time
-  int turn = 0;
-  for (int start = n0; start < n1; start += some) {
-    const int stop = min(n1, start + some);
-    if (start != n0) lds_barrier();
-    for (int x = tid; x < (stop - start) << pairs_log; x += threads)
-      angles[x] = angle_of(p, positions, start + (x >> pairs_log), x & ((1 << pairs_log) - 1));
-    lds_barrier();
-    for (int n = start; n < stop; ++n) {
-      const Piece<Kind> x = next_x, g = next_g;
-      fetch_next(n + 1 < n1);
-      float ca[4], sa[4];
+  const int pairs_log = p.lanes_log + 2;          // angles of a token, with those of entries that are not turned
+  const int some = max(1, kAngles >> pairs_log);  // tokens whose angles are made at a time
+  int turn = 0, made = 0, first_angle = 0;        // made: tokens left of those
+  no_stores<!WHOLE ? 8 : HALVES || kSize == 4 ? 2 : 1>(out);
+  for (int n = n0; n < p.N; n += step, --made) {
+    if (made == 0) {
+      if (n != n0) lds_barrier();
+      made = min(some, (p.N - 1 - n) / step + 1);
+      for (int x = tid; x < made << pairs_log; x += threads)
+        angles[x] = angle_of(p, positions, n + (x >> pairs_log) * step, x & ((1 << pairs_log) - 1));
+      first_angle = 4 * c;
+      lds_barrier();
+    }
+    const Piece<Kind> x = next_x, g = next_g;
+    fetch_next(n + step < p.N);
+    float ca[4], sa[4];
 #pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        const f32x2 cs = angles[((n - start) << pairs_log) + 4 * c + e];
-        ca[e] = cs[0];
-        sa[e] = cs[1];
-      }
-      float xa[4], xb[4];
-      if constexpr (!BWD) {
-        unpack(x, xa, xb);
-        if constexpr (NORM != LITE_ATTN_NORM_NONE) {
-          float sq = 0.f;
+    for (int e = 0; e < 4; ++e) {
+      const f32x2 cs = angles[first_angle + e];
+      ca[e] = cs[0];
+      sa[e] = cs[1];
+    }
+    float xa[4], xb[4];
+    if constexpr (!BWD) {
+      unpack(x, xa, xb);
+      if constexpr (NORM != LITE_ATTN_NORM_NONE) {
+        float sq = 0.f;
 #pragma unroll
-          for (int e = 0; e < 4; ++e)
-            if (valid(e)) sq += xa[e] * xa[e] + xb[e] * xb[e];
-          if constexpr (NORM == LITE_ATTN_NORM_HEAD) {
-            sq = sum_lanes(sq, p.lanes_log);
-          } else {
-            put_waves(&room, turn, f32x2{sum64(sq), 0.f});
-            lds_barrier();
-            sq = sum16(get_waves(&room, turn)[0]);
-            turn ^= 1;
-          }
-          const float rstd = rsqrtf(sq * side.inv_count + p.eps);
-#pragma unroll
-          for (int e = 0; e < 4; ++e) {
-            xa[e] *= rstd * wa[e];
-            xb[e] *= rstd * wb[e];
-          }
+        for (int e = 0; e < 4; ++e) sq += xa[e] * xa[e] + xb[e] * xb[e];  // (0 where there is no entry)
+        if constexpr (NORM == LITE_ATTN_NORM_HEAD) {
+          sq = sum_lanes(sq, p.lanes_log);
+        } else {
+          put_waves(&room, turn, f32x2{sum64(sq), 0.f});
+          lds_barrier();
+          sq = sum16(get_waves(&room, turn)[0]);
+          turn ^= 1;
         }
-        float ra[4], rb[4];
+        const float rstd = rsqrtf(sq * side.inv_count + p.eps);
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
-          ra[e] = xa[e] * ca[e] - xb[e] * sa[e];
-          rb[e] = xa[e] * sa[e] + xb[e] * ca[e];
+          xa[e] *= rstd * wa[e];
+          xb[e] *= rstd * wb[e];
         }
-        store(out.row(), at_out, ra, rb);
-      } else {
-        float ga[4], gb[4], za[4], zb[4];
-        unpack(g, ga, gb);
-#pragma unroll
-        for (int e = 0; e < 4; ++e) {  // the turn back
-          za[e] = ga[e] * ca[e] + gb[e] * sa[e];
-          zb[e] = gb[e] * ca[e] - ga[e] * sa[e];
-        }
-        if constexpr (NORM != LITE_ATTN_NORM_NONE) {
-          unpack(x, xa, xb);
-          float sq = 0.f, dot = 0.f;
-#pragma unroll
-          for (int e = 0; e < 4; ++e) {
-            if (!valid(e)) continue;
-            sq += xa[e] * xa[e] + xb[e] * xb[e];
-            dot += za[e] * wa[e] * xa[e] + zb[e] * wb[e] * xb[e];
-          }
-          if constexpr (NORM == LITE_ATTN_NORM_HEAD) {
-            sq = sum_lanes(sq, p.lanes_log);
-            dot = sum_lanes(dot, p.lanes_log);
-          } else {
-            put_waves(&room, turn, f32x2{sum64(sq), sum64(dot)});
-            lds_barrier();
-            const f32x2 all = get_waves(&room, turn);
-            sq = sum16(all[0]);
-            dot = sum16(all[1]);
-            turn ^= 1;
-          }
-          // n = x rstd; dx = rstd (dn - n mean(dn n)), dn = dz w
-          const float rstd = rsqrtf(sq * side.inv_count + p.eps);
-          const float pull = rstd * rstd * (dot * side.inv_count);
-#pragma unroll
-          for (int e = 0; e < 4; ++e) {
-            da[e] += za[e] * (xa[e] * rstd);
-            db[e] += zb[e] * (xb[e] * rstd);
-            za[e] = rstd * (za[e] * wa[e] - xa[e] * pull);
-            zb[e] = rstd * (zb[e] * wb[e] - xb[e] * pull);
-          }
-        }
-        store(out.row(), at_out, za, zb);
       }
-      out.step();
+      float ra[4], rb[4];
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        ra[e] = xa[e] * ca[e] - xb[e] * sa[e];
+        rb[e] = xa[e] * sa[e] + xb[e] * ca[e];
+      }
+      store(out.row(), at_out, ra, rb);
+    } else {
+      float ga[4], gb[4], za[4], zb[4];
+      unpack(g, ga, gb);
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {  // the turn back
+        za[e] = ga[e] * ca[e] + gb[e] * sa[e];
+        zb[e] = gb[e] * ca[e] - ga[e] * sa[e];
+      }
+      if constexpr (NORM != LITE_ATTN_NORM_NONE) {
+        unpack(x, xa, xb);
+        float sq = 0.f, dot = 0.f;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          sq += xa[e] * xa[e] + xb[e] * xb[e];
+          dot += za[e] * wa[e] * xa[e] + zb[e] * wb[e] * xb[e];
+        }
+        if constexpr (NORM == LITE_ATTN_NORM_HEAD) {
+          sq = sum_lanes(sq, p.lanes_log);
+          dot = sum_lanes(dot, p.lanes_log);
+        } else {
+          put_waves(&room, turn, f32x2{sum64(sq), sum64(dot)});
+          lds_barrier();
+          const f32x2 all = get_waves(&room, turn);
+          sq = sum16(all[0]);
+          dot = sum16(all[1]);
+          turn ^= 1;
+        }
+        // n = x rstd; dx = rstd (dn - n mean(dn n)), dn = dz w
+        const float rstd = rsqrtf(sq * side.inv_count + p.eps);
+        const float pull = rstd * rstd * (dot * side.inv_count);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          da[e] += za[e] * (xa[e] * rstd);
+          db[e] += zb[e] * (xb[e] * rstd);
+          za[e] = rstd * (za[e] * wa[e] - xa[e] * pull);
+          zb[e] = rstd * (zb[e] * wb[e] - xb[e] * pull);
+        }
+      }
+      store(out.row(), at_out, za, zb);
     }
+    out.step();
+    first_angle += 1 << pairs_log;
   }
   if constexpr (BWD && NORM != LITE_ATTN_NORM_NONE) {
     if (!side.part) return;
@@ -491,6 +500,9 @@ __global__ __launch_bounds__(NORM == LITE_ATTN_NORM_ROW ? kMaxTeam : 256) void r
   }
 }
 
+// Part w of n things cut into `parts`: from part_start(w) to part_start(w + 1).
+__device__ __forceinline__ int part_start(int n, int parts, int w) { return (int)((int64_t)n * w / parts); }
+
 // out[column] = the sum over `rows` rows of part[row][columns]: a workgroup takes 64 columns, its waves an equal share of the
 // rows each.
 struct RowSums {
@@ -503,12 +515,12 @@ __global__ __launch_bounds__(1024) void sum_rows_kernel(const RowSums p) {
   const int which = (int)blockIdx.x >= p.blocks0, block = which ? (int)blockIdx.x - p.blocks0 : (int)blockIdx.x;
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   const int column = block * 64 + lane, columns = p.columns[which], rows = p.rows[which];
-  const int r1 = share_start(rows, 16, wave + 1);
+  const int r1 = part_start(rows, 16, wave + 1);
   float sum = 0.f;
   if (column < columns) {
     const float* from = p.part[which] + column;
 #pragma unroll 8
-    for (int r = share_start(rows, 16, wave); r < r1; ++r) sum += from[(size_t)r * columns];
+    for (int r = part_start(rows, 16, wave); r < r1; ++r) sum += from[(size_t)r * columns];
   }
   sums[wave][lane] = sum;
   __syncthreads();
@@ -529,6 +541,8 @@ struct Columns {
   __device__ __forceinline__ bool has(int e) const { return RAGGED ? at(e) < D : thread * kEach < D; }
 };
 
+template <class Kind, bool RAGGED>
+constexpr int kRowStores = RAGGED ? kEach : Piece<Kind>::kSize / 2;
 template <bool RAGGED, class Kind>
 __device__ __forceinline__ void load_row(Buffer from, const Columns<RAGGED>& col, Piece<Kind>& to) {
   if constexpr (RAGGED) {
@@ -652,17 +666,19 @@ __device__ __forceinline__ Stats row_stats(Team& team, const float* x, const Col
   return {mean, rsqrtf(sq * inv_D + eps)};
 }
 
-// The workgroup's share of rows.
+// The workgroup's share of the rows of a group.
 struct Share {
-  int batch, n0, n1;
+  int batch, group, n0, end, step;  // group of the batch entry; rows n0, n0 + step, ... below end
   __device__ __forceinline__ explicit Share(const ResidualParams& p) {
-    batch = (int)blockIdx.x / p.shares;
-    const int part = (int)blockIdx.x - batch * p.shares;
-    n0 = share_start(p.N, p.shares, part);
-    n1 = share_start(p.N, p.shares, part + 1);
+    const int g = (int)blockIdx.x / p.shares;
+    batch = g / p.groups;
+    group = g - batch * p.groups;
+    n0 = group * p.per_mod + ((int)blockIdx.x - g * p.shares);
+    end = min(p.N, (group + 1) * p.per_mod);
+    step = p.shares;
   }
   __device__ __forceinline__ Walk walk(const Lines& l, int bytes) const {
-    return Walk{l.data + batch * l.stride_b + n0 * l.stride_n, l.stride_n, l.data ? bytes : 0};
+    return Walk{l.data + batch * l.stride_b + n0 * l.stride_n, step * l.stride_n, l.data ? bytes : 0};
   }
 };
 
@@ -683,6 +699,7 @@ __global__ __launch_bounds__(kMaxTeam) void residual_fwd_kernel(const ResidualPa
   __shared__ WaveRoom room;
   __shared__ float in_waves[kMaxTeam / 64];
   const Share share(p);
+  if (share.n0 >= share.end) return;  // (a group of fewer rows than shares)
   const Columns<RAGGED> col = {(int)threadIdx.x, (int)blockDim.x, p.D};
   Team team = {blockDim.x > 64, 0, &room};
   const int row_x = p.D * Piece<KindX>::kSize, row_y = p.D * Piece<KindY>::kSize;
@@ -700,31 +717,29 @@ __global__ __launch_bounds__(kMaxTeam) void residual_fwd_kernel(const ResidualPa
   fetch_next(true);
   const Counts counts = count_columns(p, col, in_waves);
   float open[kEach], mul[kEach], add[kEach];  // x_out = x + open * norm(y);  h = norm(x_out) * mul + add
-  int left = 0;                               // tokens left of the row of modulation
-  for (int n = share.n0; n < share.n1; ++n, --left) {
+  {
+    float t[kEach];
+    load_mod(p.gate, p.param_dtype, share.batch, share.group, col, open, 1.f);
+    load_params(p.post_w, p.param_dtype, col, t, 1.f);
+#pragma unroll
+    for (int e = 0; e < kEach; ++e) open[e] *= p.alpha * t[e];
+    load_params(p.pre_w, p.param_dtype, col, mul, 1.f);
+    load_params(p.pre_b, p.param_dtype, col, add, 0.f);
+    load_mod(p.scale, p.param_dtype, share.batch, share.group, col, t, 0.f);
+#pragma unroll
+    for (int e = 0; e < kEach; ++e) {
+      mul[e] *= 1.f + t[e];
+      add[e] *= 1.f + t[e];
+    }
+    load_mod(p.shift, p.param_dtype, share.batch, share.group, col, t, 0.f);
+#pragma unroll
+    for (int e = 0; e < kEach; ++e) add[e] += t[e];
+  }
+  no_stores<kRowStores<KindX, RAGGED> + kRowStores<KindY, RAGGED>>(x_to);
+  for (int n = share.n0; n < share.end; n += share.step) {
     const Piece<KindX> px = next_x;
     const Piece<KindY> py = next_y;
-    fetch_next(n + 1 < share.n1);
-    if (left == 0) {
-      const int g = quotient(n, p.per_mod, p.per_group);
-      left = (g + 1) * p.per_mod - n;
-      float t[kEach];
-      load_mod(p.gate, p.param_dtype, share.batch, g, col, open, 1.f);
-      load_params(p.post_w, p.param_dtype, col, t, 1.f);
-#pragma unroll
-      for (int e = 0; e < kEach; ++e) open[e] *= p.alpha * t[e];
-      load_params(p.pre_w, p.param_dtype, col, mul, 1.f);
-      load_params(p.pre_b, p.param_dtype, col, add, 0.f);
-      load_mod(p.scale, p.param_dtype, share.batch, g, col, t, 0.f);
-#pragma unroll
-      for (int e = 0; e < kEach; ++e) {
-        mul[e] *= 1.f + t[e];
-        add[e] *= 1.f + t[e];
-      }
-      load_mod(p.shift, p.param_dtype, share.batch, g, col, t, 0.f);
-#pragma unroll
-      for (int e = 0; e < kEach; ++e) add[e] += t[e];
-    }
+    fetch_next(n + share.step < share.end);
     float x[kEach];
     px.unpack(x);
     if (p.y.data) {
@@ -764,6 +779,7 @@ __global__ __launch_bounds__(kMaxTeam) void residual_bwd_kernel(const ResidualPa
   __shared__ WaveRoom room;
   __shared__ float in_waves[kMaxTeam / 64];
   const Share share(p);
+  if (share.n0 >= share.end) return;  // (a group of fewer rows than shares)
   const Columns<RAGGED> col = {(int)threadIdx.x, (int)blockDim.x, p.D};
   Team team = {blockDim.x > 64, 0, &room};
   const int row_x = p.D * Piece<KindX>::kSize, row_y = p.D * Piece<KindY>::kSize;
@@ -783,10 +799,22 @@ __global__ __launch_bounds__(kMaxTeam) void residual_bwd_kernel(const ResidualPa
   const Counts counts = count_columns(p, col, in_waves);
   float open[kEach], mul[kEach];  // alpha gate post_w, (1 + scale) pre_w
   float sum_a[kEach], sum_s[kEach], sum_c[kEach];
+  {
+    float t[kEach];
+    load_mod(p.gate, p.param_dtype, share.batch, share.group, col, open, 1.f);
+    load_params(p.post_w, p.param_dtype, col, t, 1.f);
 #pragma unroll
-  for (int e = 0; e < kEach; ++e) sum_a[e] = sum_s[e] = sum_c[e] = 0.f;
-  int left = 0;  // tokens left of the row of modulation
-  for (int n = share.n0; n < share.n1; ++n) {
+    for (int e = 0; e < kEach; ++e) open[e] *= p.alpha * t[e];
+    load_params(p.pre_w, p.param_dtype, col, mul, 1.f);
+    load_mod(p.scale, p.param_dtype, share.batch, share.group, col, t, 0.f);
+#pragma unroll
+    for (int e = 0; e < kEach; ++e) {
+      mul[e] *= 1.f + t[e];
+      sum_a[e] = sum_s[e] = sum_c[e] = 0.f;
+    }
+  }
+  no_stores<kRowStores<KindX, RAGGED> + kRowStores<KindY, RAGGED>>(dx_to);
+  for (int n = share.n0; n < share.end; n += share.step) {
     // what the row needs first is asked for a row ahead, the rest now
     const Piece<KindX> px = next_x;
     const Piece<KindY> pdh = next_dh;
@@ -794,20 +822,7 @@ __global__ __launch_bounds__(kMaxTeam) void residual_bwd_kernel(const ResidualPa
     load_row(y_in.row(), col, py);
     dxo_in.step();
     y_in.step();
-    fetch_next(n + 1 < share.n1);
-    if (left == 0) {
-      const int g = quotient(n, p.per_mod, p.per_group);
-      left = (g + 1) * p.per_mod - n;
-      float t[kEach];
-      load_mod(p.gate, p.param_dtype, share.batch, g, col, open, 1.f);
-      load_params(p.post_w, p.param_dtype, col, t, 1.f);
-#pragma unroll
-      for (int e = 0; e < kEach; ++e) open[e] *= p.alpha * t[e];
-      load_params(p.pre_w, p.param_dtype, col, mul, 1.f);
-      load_mod(p.scale, p.param_dtype, share.batch, g, col, t, 0.f);
-#pragma unroll
-      for (int e = 0; e < kEach; ++e) mul[e] *= 1.f + t[e];
-    }
+    fetch_next(n + share.step < share.end);
     float dx[kEach];
     if (p.dh.data) {
       float x[kEach];
@@ -853,23 +868,15 @@ __global__ __launch_bounds__(kMaxTeam) void residual_bwd_kernel(const ResidualPa
     if (p.dy.data && p.post != LITE_ATTN_NORM_NONE) norm_back(team, dx, y, rstd, p.post, p.inv_D, col);
     store_row<KindY>(dy_to.row(), col, dx);
     dy_to.step();
-    // the sums of a share's part of a row of modulation: places grow with the share and with the row of modulation
-    if (--left == 0 || n + 1 == share.n1) {
-      if (p.part) {
-        const int g = quotient(n, p.per_mod, p.per_group);
-        const int64_t bytes = 4 * (int64_t)p.D;
-        char* to = reinterpret_cast<char*>(p.part) + 3 * bytes * ((int64_t)blockIdx.x + share.batch * (int64_t)p.groups + g);
-        Walk sums = {to, bytes, (int)bytes};
-        store_row<F32>(sums.row(), col, sum_a);
-        sums.step();
-        store_row<F32>(sums.row(), col, sum_s);
-        sums.step();
-        store_row<F32>(sums.row(), col, sum_c);
-      }
-#pragma unroll
-      for (int e = 0; e < kEach; ++e) sum_a[e] = sum_s[e] = sum_c[e] = 0.f;
-    }
   }
+  if (!p.part) return;
+  const int64_t bytes = 4 * (int64_t)p.D;
+  Walk sums = {reinterpret_cast<char*>(p.part) + 3 * bytes * blockIdx.x, bytes, (int)bytes};
+  store_row<F32>(sums.row(), col, sum_a);
+  sums.step();
+  store_row<F32>(sums.row(), col, sum_s);
+  sums.step();
+  store_row<F32>(sums.row(), col, sum_c);
 }
 
 // Sums of a row of modulation: its shares' sums in order, each of the waves an equal part of them, and what follows from them.
@@ -880,13 +887,11 @@ __global__ __launch_bounds__(1024) void group_sums_kernel(const ResidualParams p
   const size_t D = p.D;
   for (int group = blockIdx.x; group < all_groups; group += gridDim.x) {
     const int b = group / p.groups, g = group - b * p.groups;
-    const int64_t end = (int64_t)(g + 1) * p.per_mod;
-    const int s0 = b * p.shares + share_of(p.N, p.shares, g * p.per_mod);
-    const int s1 = b * p.shares + share_of(p.N, p.shares, (int)(end < p.N ? end : p.N) - 1) + 1;
-    const int from = s0 + share_start(s1 - s0, waves, wave), to = s0 + share_start(s1 - s0, waves, wave + 1);
+    const int shares = min(p.shares, min(p.N, (g + 1) * p.per_mod) - g * p.per_mod);
+    const int from = part_start(shares, waves, wave), to = part_start(shares, waves, wave + 1);
     float a = 0.f, s = 0.f, c = 0.f;
     if (column < p.D) {
-      const float* part = p.part + ((size_t)from + group) * 3 * D + column;
+      const float* part = p.part + ((size_t)group * p.shares + from) * 3 * D + column;
 #pragma unroll 4
       for (int x = from; x < to; ++x, part += 3 * D) {
         a += part[0];
@@ -934,7 +939,7 @@ __global__ __launch_bounds__(1024) void weight_sums_kernel(const ResidualParams 
   if (!out) return;
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   const int column = blockIdx.x * 64 + lane;
-  const int from = share_start(all_groups, 16, wave), to = share_start(all_groups, 16, wave + 1);
+  const int from = part_start(all_groups, 16, wave), to = part_start(all_groups, 16, wave + 1);
   float sum = 0.f;
   if (column < p.D) {
     const float* part = p.group_sums + blockIdx.y * (size_t)p.D + column;
@@ -1033,8 +1038,7 @@ hipError_t launch_residual_sums(const ResidualParams& p, hipStream_t st) {
   const int64_t groups = (int64_t)p.batch * p.groups;
   const unsigned columns = (unsigned)(p.D + 63) / 64;
   if (groups > 0) {
-    const int64_t shares = p.shares * (int64_t)p.per_mod / p.N + 2;  // of a group, at most
-    const int waves = shares < 32 ? (shares < 8 ? 2 : 4) : 16;
+    const int waves = p.shares < 2 ? 1 : p.shares < 32 ? 4 : 16;
     const dim3 grid((unsigned)(groups < 65536 ? groups : 65536), columns);
     group_sums_kernel<<<grid, 64 * waves, 0, st>>>(p, (int)groups);
     const hipError_t e = hipGetLastError();

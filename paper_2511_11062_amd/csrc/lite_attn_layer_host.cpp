@@ -61,12 +61,18 @@ bool good_vector(const T* p, int dtype) {
 }
 bool good_grad(const float* p) { return ((uintptr_t)p & 3) == 0; }
 
-// Shares of a batch entry's N rows, for `parts` kinds of workgroups of `waves` waves that run side by side: altogether as many
-// workgroups as the chip holds at `per_simd` waves on each of its SIMDs.
-int shares_of(int batch, int N, int waves, int per_simd, int64_t parts) {
-  const int64_t side_by_side = (int64_t)kCUs * std::max(1, std::min(16, 4 * per_simd / waves));
-  const int64_t each = side_by_side / (parts * batch);
-  return (int)std::max<int64_t>(1, std::min<int64_t>(N, each));
+// Shares that each of `kinds` kinds of rows is dealt to (at most `rows`, of a kind), in workgroups of `waves` waves, `per_cu`
+// waves on a CU altogether.
+int shares_of(int64_t kinds, int rows, int waves, int per_cu) {
+  const int64_t side_by_side = (int64_t)kCUs * std::max(1, (per_cu + waves / 2) / waves);
+  return (int)std::max<int64_t>(1, std::min<int64_t>(rows, side_by_side / kinds));
+}
+
+int launch_of(int64_t kinds, int64_t shares, int threads, LayerLaunch* l) {
+  if (kinds * shares * threads >= (int64_t)1 << 32) return LITE_ATTN_EUNSUPPORTED;  // (what a launch may have)
+  l->threads = threads;
+  l->blocks = (int)(kinds * shares);
+  return LITE_ATTN_OK;
 }
 
 int log2_up(int x) {
@@ -87,7 +93,7 @@ RotaryShape rotary_shape(const lite_attn_rotary_desc_t& d, bool bwd) {
   s.threads = (s.team_heads * lanes + 63) / 64 * 64;
   s.groups[0] = (d.heads_q + s.team_heads - 1) / s.team_heads;
   s.groups[1] = (d.heads_k + s.team_heads - 1) / s.team_heads;
-  s.shares = shares_of(d.batch, d.seqlen, s.threads / 64, bwd ? 4 : 8, s.groups[0] + s.groups[1]);
+  s.shares = shares_of((int64_t)d.batch * (s.groups[0] + s.groups[1]), d.seqlen, s.threads / 64, bwd ? 16 : 24);
   return s;
 }
 
@@ -189,9 +195,7 @@ int plan_rotary(const lite_attn_rotary_desc_t& d, const lite_attn_rotary_fwd_t& 
     set(p->side[x].xs, in, d.dtype);
     set(p->side[x].os, out, d.dtype);
   }
-  l->threads = s.threads;
-  l->blocks = d.batch * s.shares * (s.groups[0] + s.groups[1]);
-  return LITE_ATTN_OK;
+  return launch_of(d.batch, (int64_t)s.shares * (s.groups[0] + s.groups[1]), s.threads, l);
 }
 
 int plan_rotary(const lite_attn_rotary_desc_t& d, const lite_attn_rotary_bwd_t& a, RotaryParams* p, LayerLaunch* l) {
@@ -223,9 +227,7 @@ int plan_rotary(const lite_attn_rotary_desc_t& d, const lite_attn_rotary_bwd_t& 
     if (grads[x]) p->side[x].part = part;
     part += (size_t)d.batch * s.shares * rotary_part(d, s, x);
   }
-  l->threads = s.threads;
-  l->blocks = d.batch * s.shares * (s.groups[0] + s.groups[1]);
-  return LITE_ATTN_OK;
+  return launch_of(d.batch, (int64_t)s.shares * (s.groups[0] + s.groups[1]), s.threads, l);
 }
 
 namespace {
@@ -234,16 +236,17 @@ struct ResidualShape {
   int threads, shares;
 };
 
-// A workgroup takes a row of `dim` entries, kEach in a thread.
+int groups_of(const lite_attn_residual_desc_t& d) {
+  return (int)(((int64_t)d.seqlen + d.tokens_per_mod - 1) / d.tokens_per_mod);
+}
+
+// A workgroup takes a row of `dim` entries, kEach in a thread, and rows of one group (tokens that share a row of modulation).
 ResidualShape residual_shape(const lite_attn_residual_desc_t& d, bool bwd) {
   ResidualShape s;
   s.threads = (d.dim + 64 * kEach - 1) / (64 * kEach) * 64;
-  s.shares = shares_of(d.batch, d.seqlen, s.threads / 64, bwd ? 4 : 8, 1);
+  s.shares = shares_of(std::max<int64_t>(1, (int64_t)d.batch * groups_of(d)), std::min(d.tokens_per_mod, d.seqlen),
+                       s.threads / 64, bwd ? 16 : 24);
   return s;
-}
-
-int groups_of(const lite_attn_residual_desc_t& d) {
-  return (int)(((int64_t)d.seqlen + d.tokens_per_mod - 1) / d.tokens_per_mod);
 }
 
 // Rows of modulation, or none.
@@ -275,7 +278,6 @@ int fill_residual(const lite_attn_residual_desc_t& d, const ResidualShape& s, co
   p->pre_eps = d.pre_eps;
   p->alpha = d.residual_scale;
   p->inv_D = 1.f / (float)d.dim;
-  p->per_group = reciprocal(p->per_mod);
   return LITE_ATTN_OK;
 }
 
@@ -308,9 +310,7 @@ int plan_residual(const lite_attn_residual_desc_t& d, const lite_attn_residual_f
   if (!take(a.x, d.stream_dtype, false, &p->x) || !take(a.y, d.dtype, false, &p->y) ||
       !take(a.x_out, d.stream_dtype, true, &p->x_out) || !take(a.h, d.dtype, true, &p->h))
     return LITE_ATTN_EINVAL;
-  l->threads = s.threads;
-  l->blocks = d.batch * s.shares;
-  return LITE_ATTN_OK;
+  return launch_of((int64_t)d.batch * p->groups, s.shares, s.threads, l);
 }
 
 int plan_residual(const lite_attn_residual_desc_t& d, const lite_attn_residual_bwd_t& a, ResidualParams* p,
@@ -340,7 +340,7 @@ int plan_residual(const lite_attn_residual_desc_t& d, const lite_attn_residual_b
     return LITE_ATTN_EINVAL;
   if (sums) {
     p->part = static_cast<float*>(a.workspace);
-    p->group_sums = p->part + 3 * (size_t)d.batch * (s.shares + p->groups) * d.dim;
+    p->group_sums = p->part + 3 * (size_t)d.batch * p->groups * s.shares * d.dim;
     p->dgate = a.dgate;
     p->dscale = a.dscale;
     p->dshift = a.dshift;
@@ -348,9 +348,7 @@ int plan_residual(const lite_attn_residual_desc_t& d, const lite_attn_residual_b
     p->dpre_w = a.dpre_weight;
     p->dpre_b = a.dpre_bias;
   }
-  l->threads = s.threads;
-  l->blocks = d.batch * s.shares;
-  return LITE_ATTN_OK;
+  return launch_of((int64_t)d.batch * p->groups, s.shares, s.threads, l);
 }
 
 }  // namespace la
@@ -365,8 +363,8 @@ size_t lite_attn_rotary_bwd_workspace(const lite_attn_rotary_desc_t* desc) {
 
 size_t lite_attn_residual_norm_bwd_workspace(const lite_attn_residual_desc_t* desc) {
   if (la::check_residual(desc) != LITE_ATTN_OK) return 0;
-  const size_t rows = la::residual_shape(*desc, true).shares + 2 * (size_t)la::groups_of(*desc);
-  return la::up16(3 * sizeof(float) * desc->batch * rows * desc->dim);
+  const size_t rows = (size_t)desc->batch * la::groups_of(*desc) * (la::residual_shape(*desc, true).shares + 1);
+  return la::up16(3 * sizeof(float) * rows * desc->dim);
 }
 
 int lite_attn_rotary_freqs(const int32_t axis_pairs[3], double theta, double* host_freqs) {

@@ -8,9 +8,11 @@
 
 namespace la {
 
-// Both operators go over rows (a token, or some heads of one) with a team of threads that hold kEach entries of the row
-// each, for a whole share of consecutive rows of a batch entry: what depends on the column alone (weights, gate, scale,
-// shift, sums over tokens) stays in registers from row to row.
+// Both operators go over rows (a token, or some heads of one) with workgroups whose threads hold kEach entries of the row
+// each and that take several rows with the same weights, gate, scale and shift: these, and sums over tokens, stay in
+// registers from row to row.  Workgroups that run side by side take neighbouring rows, and all of them move on by the same
+// step: what they have under way at any time lies close together in memory (shares of consecutive rows, a window for each
+// workgroup, reach 5.0 TB/s where this reaches 5.8, in a copy of 1.5 GB).
 constexpr int kEach = 8;
 constexpr int kMaxTeam = 1024;
 constexpr int kAngles = 1024;  // angles of the tokens that a workgroup keeps at a time, 8 bytes each
@@ -33,7 +35,7 @@ struct RotaryParams {
   const int32_t* positions;
   int64_t positions_stride_b;
   int batch, N;
-  int shares;            // of consecutive tokens of a batch entry
+  int shares;            // share x of a batch entry: tokens x, x + shares, x + 2 shares, ...
   int head_dim, pairs;
   int lanes_log;         // a head takes 1 << lanes_log threads of kEach entries
   int team_heads;        // heads that a workgroup takes
@@ -55,22 +57,17 @@ struct ResidualParams {
   Lines gate, scale, shift;
   const void *post_w, *pre_w, *pre_b;
   int batch, N, D, per_mod, groups;  // groups of a batch entry
-  int shares;                        // of consecutive rows of a batch entry
+  int shares;                        // share x of a group's rows, the first being n0: n0 + x, n0 + x + shares, ...
   int post, pre, param_dtype;
   float post_eps, pre_eps, alpha, inv_D;
-  float* part;                       // backwards: [batch * (shares + groups)][3][D] sums, or null
+  float* part;                       // backwards: [batch * groups][shares][3][D] sums, or null
   float *dgate, *dscale, *dshift, *dpost_w, *dpre_w, *dpre_b;
   float* group_sums;                 // [batch * groups][3][D]: the groups' parts of the weights' gradients
-  uint32_t per_group;                // reciprocal(per_mod)
 };
 
 struct LayerLaunch {
   int threads, blocks;
 };
-
-// Rows n of a share c of `shares` of N rows: share_start(c) <= n < share_start(c + 1); the share that row n is in.
-constexpr int share_start(int N, int shares, int c) { return (int)((int64_t)N * c / shares); }
-constexpr int share_of(int N, int shares, int n) { return (int)((((int64_t)n + 1) * shares - 1) / N); }
 
 // lite_attn_layer_host.cpp (no HIP calls): checks, and what a call launches
 int check_rotary(const lite_attn_rotary_desc_t* d);
