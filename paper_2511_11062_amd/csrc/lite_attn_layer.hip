@@ -14,6 +14,8 @@
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 
+#include <type_traits>
+
 #include "lite_attn_kernels.h"
 #include "lite_attn_layer_kernels.h"
 
@@ -219,28 +221,31 @@ __device__ __forceinline__ f32x2 get_waves(const WaveRoom* room, int turn) {
 
 // ---- rotary positions --------------------------------------------------------------------------------------------------
 
-// cos and sin of a pair's angle at token n of a batch entry, whose positions are given or null.  In 64 bits until whole turns
-// are off: in 32 an angle of 10^5 radians would be off by 6e-3.
-__device__ __forceinline__ f32x2 angle_of(const RotaryParams& p, const int32_t* positions, int n, int pair) {
-  if (pair >= p.pairs) return f32x2{1.f, 0.f};
-  double p0, p1, p2;
-  if (positions) {
-    p0 = positions[n];
-    p1 = positions[n + (int64_t)p.N];
-    p2 = positions[n + 2 * (int64_t)p.N];
-  } else {
-    int t = p.token_start + n;
-    if (t >= p.video) t = 0;
-    const int f = quotient(t, p.area, p.per_area), in = t - f * p.area;
-    const int y = quotient(in, p.width, p.per_width);
-    p0 = f;
-    p1 = y;
-    p2 = in - y * p.width;
-  }
-  const double* f = p.freqs + pair;
-  double turns = p0 * f[0];
-  turns = __builtin_fma(p1, f[p.pairs], turns);
-  turns = __builtin_fma(p2, f[2 * p.pairs], turns);
+// Where a token stands.
+struct Position {
+  int at[3];
+};
+__device__ __forceinline__ Position position_of(const RotaryParams& p, const int32_t* positions, int n) {
+  if (positions) return {{positions[n], positions[n + (int64_t)p.N], positions[n + 2 * (int64_t)p.N]}};
+  int t = p.token_start + n;
+  if (t >= p.video) t = 0;
+  const int f = quotient(t, p.area, p.per_area), in = t - f * p.area, y = quotient(in, p.width, p.per_width);
+  return {{f, y, in - y * p.width}};
+}
+
+// How fast a pair turns, and its cos and sin at a position.  In 64 bits until whole turns are off: in 32 an angle of 10^5
+// radians would be off by 6e-3.
+struct Speed {
+  double f[3];
+};
+__device__ __forceinline__ Speed speed_of(const RotaryParams& p, int pair) {
+  if (pair >= p.pairs) return {{0.0, 0.0, 0.0}};
+  return {{p.freqs[pair], p.freqs[p.pairs + pair], p.freqs[2 * p.pairs + pair]}};
+}
+__device__ __forceinline__ f32x2 angle_of(const Speed& v, const Position& at) {
+  double turns = (double)at.at[0] * v.f[0];
+  turns = __builtin_fma((double)at.at[1], v.f[1], turns);
+  turns = __builtin_fma((double)at.at[2], v.f[2], turns);
   turns *= 0.15915494309189533577;  // 1 / (2 pi)
   turns -= __builtin_rint(turns);
   float s, c;
@@ -248,28 +253,47 @@ __device__ __forceinline__ f32x2 angle_of(const RotaryParams& p, const int32_t* 
   return f32x2{c, s};
 }
 
-// A workgroup: some heads (under NORM_ROW all) of q or k, for a share of consecutive rows, a row being a token.  A thread
-// holds four pairs of a head, a[4] and b[4].  WHOLE: they are eight entries in a row or, of turned halves, four and four;
-// otherwise (a head's ragged end, four pairs across the end of the turned halves) every entry is fetched by itself.
+// The angles of `count` tokens n, n + step, ..., 1 << pairs_log for each.  If those are whole waves, a wave takes a token, whose
+// position it finds by scalar instructions, and a thread keeps its pair.
+__device__ __forceinline__ void make_angles(const RotaryParams& p, const int32_t* positions, int n, int step, int count,
+                                            int pairs_log, f32x2* angles) {
+  if (pairs_log >= 6) {
+    const int waves = blockDim.x >> 6, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
+    for (int first = 0; first < 1 << pairs_log; first += 64) {
+      const Speed v = speed_of(p, first + lane);
+      for (int x = wave; x < count; x += waves)
+        angles[(x << pairs_log) + first + lane] = angle_of(v, position_of(p, positions, n + x * step));
+    }
+  } else {
+    for (int x = threadIdx.x; x < count << pairs_log; x += blockDim.x)
+      angles[x] = angle_of(speed_of(p, x & ((1 << pairs_log) - 1)), position_of(p, positions, n + (x >> pairs_log) * step));
+  }
+}
+
+// A workgroup: some heads (under NORM_ROW all) of q and the same heads of k, whose angles are the same, for a share of the
+// tokens.  A row is a token's heads of q or of k, one after the other.  (Backwards through a norm, where weights and the sums
+// for their gradient would need 32 registers, a workgroup takes q or k.)  A thread holds four pairs of a head, a[4] and b[4].
+// WHOLE: they are eight entries in a row or, of turned halves, four and four; otherwise (a head's ragged end, four pairs across
+// the end of the turned halves) every entry is fetched by itself.
 template <class Kind, bool HALVES, bool WHOLE, int NORM, bool BWD>
 __global__ __launch_bounds__(NORM == LITE_ATTN_NORM_ROW ? kMaxTeam : 256) void rotary_kernel(const RotaryParams p) {
   constexpr int kSize = Piece<Kind>::kSize;
+  constexpr bool kNormed = NORM != LITE_ATTN_NORM_NONE;
+  constexpr int kSides = rotary_sides(NORM, BWD);
   __shared__ f32x2 angles[kAngles];
   __shared__ WaveRoom room;
-  const int tid = threadIdx.x, threads = blockDim.x;
-  const int parts = p.side[0].groups + p.side[1].groups;
-  const int share = (int)(blockIdx.x / (unsigned)parts), part = (int)(blockIdx.x - share * (unsigned)parts);
+  const int tid = threadIdx.x;
+  const int block = kSides == 2 ? (int)blockIdx.x : (int)blockIdx.x / p.sides;
+  const RotarySide* const sides = p.side + (kSides == 2 ? 0 : (int)blockIdx.x - block * p.sides);
+  const int share = block / p.groups, group = block - share * p.groups;
   const int batch = share / p.shares, n0 = share - batch * p.shares, step = p.shares;
-  const int which = part >= p.side[0].groups;
-  const RotarySide& side = p.side[which];
-  const int group = which ? part - p.side[0].groups : part;
 
   const int lanes = 1 << p.lanes_log;
   const int slot = tid >> p.lanes_log, c = tid & (lanes - 1);
   const int head = group * p.team_heads + slot;
   // pairs of the head from this thread's first on
-  const int count = slot < p.team_heads && head < side.heads ? min(4, p.head_dim / 2 - 4 * c) : 0;
-  auto valid = [&](int e) { return WHOLE ? count > 0 : e < count; };
+  const int in_head = slot < p.team_heads ? min(4, p.head_dim / 2 - 4 * c) : 0;
+  auto valid = [&](int side, int e) { return head < sides[side].heads && (WHOLE ? in_head > 0 : e < in_head); };
   // places in the head of a[e] and b[e]
   const int P = p.pairs;
   auto place_a = [&](int e) {
@@ -282,28 +306,33 @@ __global__ __launch_bounds__(NORM == LITE_ATTN_NORM_ROW ? kMaxTeam : 256) void r
 
   // A wave's rows start at its first head; its other heads are `stride_h` apart.  Entries that are not there lie behind all.
   const int wave_slot = __builtin_amdgcn_readfirstlane(slot), wave_head = group * p.team_heads + wave_slot;
-  auto walk = [&](const char* data, const int64_t* s) {
-    const int span = (int)(min(63 >> p.lanes_log, side.heads - 1) * s[1]) + p.head_dim * kSize;
-    return Walk{const_cast<char*>(data) + batch * s[0] + n0 * s[2] + wave_head * s[1], step * s[2], span};
+  struct Tensor {
+    Walk walk;
+    int first, second;
   };
-  struct Places {
-    int first, second, missing;
+  auto tensor = [&](int side, const char* data, const int64_t* s) {
+    Tensor t;
+    const int heads = sides[side].heads;
+    const int span = heads == 0 ? 0 : (int)(min(63 >> p.lanes_log, heads - 1) * s[1]) + p.head_dim * kSize;
+    t.walk = Walk{const_cast<char*>(data) + batch * s[0] + n0 * s[2] + wave_head * s[1], step * s[2], span};
+    const int at = (slot - wave_slot) * (int)s[1];
+    t.first = valid(side, 0) ? at + first * kSize : span;
+    t.second = valid(side, 0) ? at + second * kSize : span;
+    return t;
   };
-  auto places = [&](const Walk& w, int64_t stride_h) {
-    const int at = (slot - wave_slot) * (int)stride_h;
-    return count > 0 ? Places{at + first * kSize, at + second * kSize, w.bytes} : Places{w.bytes, w.bytes, w.bytes};
-  };
-  auto fetch = [&](Buffer from, const Places& at, Piece<Kind>& to) {
+  auto fetch = [&](int side, Tensor& t, bool there, Piece<Kind>& to) {
+    const Buffer from = t.walk.row_if(there);
+    t.walk.step();
     if constexpr (WHOLE && HALVES) {
-      to.load_run(0, from, at.first);
-      to.load_run(1, from, at.second);
+      to.load_run(0, from, t.first);
+      to.load_run(1, from, t.second);
     } else if constexpr (WHOLE) {
-      to.load(from, at.first);
+      to.load(from, t.first);
     } else {
 #pragma unroll
       for (int e = 0; e < 4; ++e) {
-        const int a = valid(e) ? at.first + (place_a(e) - first) * kSize : at.missing;
-        const int b = valid(e) ? at.first + (place_b(e) - first) * kSize : at.missing;
+        const int a = valid(side, e) ? t.first + (place_a(e) - first) * kSize : t.walk.bytes;
+        const int b = valid(side, e) ? t.first + (place_b(e) - first) * kSize : t.walk.bytes;
         to.load_two(2 * e, from, a, b);
       }
     }
@@ -317,7 +346,9 @@ __global__ __launch_bounds__(NORM == LITE_ATTN_NORM_ROW ? kMaxTeam : 256) void r
       b[e] = WHOLE && HALVES && apart ? x[4 + e] : x[2 * e + 1];
     }
   };
-  auto store = [&](Buffer to, const Places& at, const float* ra, const float* rb) {
+  auto store = [&](int side, Tensor& t, const float* ra, const float* rb) {
+    const Buffer to = t.walk.row();
+    t.walk.step();
     float x[kEach];
 #pragma unroll
     for (int e = 0; e < kEach; ++e) {
@@ -327,74 +358,66 @@ __global__ __launch_bounds__(NORM == LITE_ATTN_NORM_ROW ? kMaxTeam : 256) void r
     Piece<Kind> out;
     out.pack(x);
     if constexpr (WHOLE && HALVES) {
-      out.store_run(0, to, at.first);
-      out.store_run(1, to, at.second);
+      out.store_run(0, to, t.first);
+      out.store_run(1, to, t.second);
     } else if constexpr (WHOLE) {
-      out.store(to, at.first);
+      out.store(to, t.first);
     } else {
 #pragma unroll
       for (int e = 0; e < 4; ++e) {
-        const int a = valid(e) ? at.first + (place_a(e) - first) * kSize : at.missing;
-        const int b = valid(e) ? at.first + (place_b(e) - first) * kSize : at.missing;
+        const int a = valid(side, e) ? t.first + (place_a(e) - first) * kSize : t.walk.bytes;
+        const int b = valid(side, e) ? t.first + (place_b(e) - first) * kSize : t.walk.bytes;
         out.store_two(2 * e, to, a, b);
       }
     }
   };
 
-  float wa[4], wb[4], da[4], db[4];  // weights and, backwards, the sums for their gradient
-  if constexpr (NORM != LITE_ATTN_NORM_NONE) {
+  Tensor in_x[kSides], in_g[kSides], out[kSides];
 #pragma unroll
-    for (int e = 0; e < 4; ++e) {
-      wa[e] = wb[e] = 1.f;
-      da[e] = db[e] = 0.f;
-      if (side.w && valid(e)) {
-        const int row = NORM == LITE_ATTN_NORM_ROW ? head * p.head_dim : 0;
-        wa[e] = load_param(side.w, p.weight_dtype, row + place_a(e));
-        wb[e] = load_param(side.w, p.weight_dtype, row + place_b(e));
+  for (int side = 0; side < kSides; ++side) {
+    const RotarySide& s = sides[side];
+    if constexpr (!BWD || kNormed) in_x[side] = tensor(side, s.x, s.xs);
+    if constexpr (BWD) in_g[side] = tensor(side, s.g, s.gs);
+    out[side] = tensor(side, s.out, s.os);
+  }
+  Piece<Kind> next_x, next_g;
+  auto fetch_next = [&](int side, bool there) {
+    if constexpr (!BWD || kNormed) fetch(side, in_x[side], there, next_x);
+    if constexpr (BWD) fetch(side, in_g[side], there, next_g);
+  };
+  fetch_next(0, true);
+  float wa[kSides][4], wb[kSides][4], da[kSides][4], db[kSides][4];  // weights and, backwards, the sums for their gradient
+  if constexpr (kNormed) {
+#pragma unroll
+    for (int side = 0; side < kSides; ++side) {
+      const void* w = sides[side].w;
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        wa[side][e] = wb[side][e] = 1.f;
+        da[side][e] = db[side][e] = 0.f;
+        if (w && valid(side, e)) {
+          const int row = NORM == LITE_ATTN_NORM_ROW ? head * p.head_dim : 0;
+          wa[side][e] = load_param(w, p.weight_dtype, row + place_a(e));
+          wb[side][e] = load_param(w, p.weight_dtype, row + place_b(e));
+        }
       }
     }
   }
-  Walk in_x = walk(side.x, side.xs), in_g = walk(side.g, side.gs), out = walk(side.out, side.os);
-  const Places at_x = places(in_x, side.xs[1]), at_g = places(in_g, side.gs[1]), at_out = places(out, side.os[1]);
-  Piece<Kind> next_x, next_g;
-  auto fetch_next = [&](bool there) {
-    if constexpr (!BWD || NORM != LITE_ATTN_NORM_NONE) {
-      fetch(in_x.row_if(there), at_x, next_x);
-      in_x.step();
-    }
-    if constexpr (BWD) {
-      fetch(in_g.row_if(there), at_g, next_g);
-      in_g.step();
-    }
-  };
-  fetch_next(true);
-  const int32_t* positions = p.positions ? p.positions + batch * p.positions_stride_b : nullptr;
-  const int pairs_log = p.lanes_log + 2;          // angles of a token, with those of entries that are not turned
-  const int some = max(1, kAngles >> pairs_log);  // tokens whose angles are made at a time
-  int turn = 0, made = 0, first_angle = 0;        // made: tokens left of those
-  no_stores<!WHOLE ? 8 : HALVES || kSize == 4 ? 2 : 1>(out);
-  for (int n = n0; n < p.N; n += step, --made) {
-    if (made == 0) {
-      if (n != n0) lds_barrier();
-      made = min(some, (p.N - 1 - n) / step + 1);
-      for (int x = tid; x < made << pairs_log; x += threads)
-        angles[x] = angle_of(p, positions, n + (x >> pairs_log) * step, x & ((1 << pairs_log) - 1));
-      first_angle = 4 * c;
-      lds_barrier();
-    }
+  int turn = 0;
+  float ca[4], sa[4];
+  // A row; the next one is of `next_side`.
+  auto do_row = [&](auto index, int next_side, bool there) {
+    constexpr int side = decltype(index)::value;
     const Piece<Kind> x = next_x, g = next_g;
-    fetch_next(n + step < p.N);
-    float ca[4], sa[4];
-#pragma unroll
-    for (int e = 0; e < 4; ++e) {
-      const f32x2 cs = angles[first_angle + e];
-      ca[e] = cs[0];
-      sa[e] = cs[1];
-    }
+    if (kSides == 2 && next_side)
+      fetch_next(kSides - 1, there);
+    else
+      fetch_next(0, there);
+    const float inv_count = sides[side].inv_count;
     float xa[4], xb[4];
     if constexpr (!BWD) {
       unpack(x, xa, xb);
-      if constexpr (NORM != LITE_ATTN_NORM_NONE) {
+      if constexpr (kNormed) {
         float sq = 0.f;
 #pragma unroll
         for (int e = 0; e < 4; ++e) sq += xa[e] * xa[e] + xb[e] * xb[e];  // (0 where there is no entry)
@@ -406,11 +429,11 @@ __global__ __launch_bounds__(NORM == LITE_ATTN_NORM_ROW ? kMaxTeam : 256) void r
           sq = sum16(get_waves(&room, turn)[0]);
           turn ^= 1;
         }
-        const float rstd = rsqrtf(sq * side.inv_count + p.eps);
+        const float rstd = rsqrtf(sq * inv_count + p.eps);
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
-          xa[e] *= rstd * wa[e];
-          xb[e] *= rstd * wb[e];
+          xa[e] *= rstd * wa[side][e];
+          xb[e] *= rstd * wb[side][e];
         }
       }
       float ra[4], rb[4];
@@ -419,7 +442,7 @@ __global__ __launch_bounds__(NORM == LITE_ATTN_NORM_ROW ? kMaxTeam : 256) void r
         ra[e] = xa[e] * ca[e] - xb[e] * sa[e];
         rb[e] = xa[e] * sa[e] + xb[e] * ca[e];
       }
-      store(out.row(), at_out, ra, rb);
+      store(side, out[side], ra, rb);
     } else {
       float ga[4], gb[4], za[4], zb[4];
       unpack(g, ga, gb);
@@ -428,13 +451,13 @@ __global__ __launch_bounds__(NORM == LITE_ATTN_NORM_ROW ? kMaxTeam : 256) void r
         za[e] = ga[e] * ca[e] + gb[e] * sa[e];
         zb[e] = gb[e] * ca[e] - ga[e] * sa[e];
       }
-      if constexpr (NORM != LITE_ATTN_NORM_NONE) {
+      if constexpr (kNormed) {
         unpack(x, xa, xb);
         float sq = 0.f, dot = 0.f;
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
           sq += xa[e] * xa[e] + xb[e] * xb[e];
-          dot += za[e] * wa[e] * xa[e] + zb[e] * wb[e] * xb[e];
+          dot += za[e] * wa[side][e] * xa[e] + zb[e] * wb[side][e] * xb[e];
         }
         if constexpr (NORM == LITE_ATTN_NORM_HEAD) {
           sq = sum_lanes(sq, p.lanes_log);
@@ -448,52 +471,83 @@ __global__ __launch_bounds__(NORM == LITE_ATTN_NORM_ROW ? kMaxTeam : 256) void r
           turn ^= 1;
         }
         // n = x rstd; dx = rstd (dn - n mean(dn n)), dn = dz w
-        const float rstd = rsqrtf(sq * side.inv_count + p.eps);
-        const float pull = rstd * rstd * (dot * side.inv_count);
+        const float rstd = rsqrtf(sq * inv_count + p.eps);
+        const float pull = rstd * rstd * (dot * inv_count);
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
-          da[e] += za[e] * (xa[e] * rstd);
-          db[e] += zb[e] * (xb[e] * rstd);
-          za[e] = rstd * (za[e] * wa[e] - xa[e] * pull);
-          zb[e] = rstd * (zb[e] * wb[e] - xb[e] * pull);
+          da[side][e] += za[e] * (xa[e] * rstd);
+          db[side][e] += zb[e] * (xb[e] * rstd);
+          za[e] = rstd * (za[e] * wa[side][e] - xa[e] * pull);
+          zb[e] = rstd * (zb[e] * wb[side][e] - xb[e] * pull);
         }
       }
-      store(out.row(), at_out, za, zb);
+      store(side, out[side], za, zb);
     }
-    out.step();
-    first_angle += 1 << pairs_log;
-  }
-  if constexpr (BWD && NORM != LITE_ATTN_NORM_NONE) {
-    if (!side.part) return;
-    if constexpr (NORM == LITE_ATTN_NORM_ROW) {
-      float* to = side.part + ((size_t)share * side.heads + head) * p.head_dim;
-#pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        if (!valid(e)) continue;
-        to[place_a(e)] = da[e];
-        to[place_b(e)] = db[e];
-      }
-    } else {  // the heads share their weights: summed in order here, a head's sums after the other's
-      __shared__ float sums[256 * kEach];
-      const int padded = lanes * kEach;
-#pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        sums[tid * kEach + 2 * e] = valid(e) ? da[e] : 0.f;
-        sums[tid * kEach + 2 * e + 1] = valid(e) ? db[e] : 0.f;
-      }
+  };
+
+  const int32_t* positions = p.positions ? p.positions + batch * p.positions_stride_b : nullptr;
+  const int pairs_log = p.lanes_log + 2;          // angles of a token, with those of entries that are not turned
+  const int some = max(1, kAngles >> pairs_log);  // tokens whose angles are made at a time
+  const bool both = kSides == 2 && p.sides == 2;
+  int made = 0, at = 0;  // tokens left of those, and where this one's start
+  no_stores<!WHOLE ? 8 : HALVES || kSize == 4 ? 2 : 1>(out[0].walk);
+  for (int n = n0; n < p.N; n += step) {
+    if (made == 0) {
+      if (n != n0) lds_barrier();
+      made = min(some, (p.N - 1 - n) / step + 1);
+      make_angles(p, positions, n, step, made, pairs_log, angles);
+      at = 4 * c;
       lds_barrier();
-      float* to = side.part + ((size_t)share * side.groups + group) * p.head_dim;
-      if (slot == 0) {
+    }
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      const f32x2 cs = angles[at + e];
+      ca[e] = cs[0];
+      sa[e] = cs[1];
+    }
+    at += 1 << pairs_log;
+    --made;
+    const bool more = n + step < p.N;
+    do_row(std::integral_constant<int, 0>{}, both, both || more);
+    if (both) do_row(std::integral_constant<int, kSides - 1>{}, 0, more);
+  }
+
+  if constexpr (BWD && kNormed) {
+#pragma unroll
+    for (int side = 0; side < kSides; ++side) {
+      const RotarySide& s = sides[side];
+      if (!s.part) continue;
+      if constexpr (NORM == LITE_ATTN_NORM_ROW) {
+        float* to = s.part + ((size_t)share * s.heads + head) * p.head_dim;
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
-          if (!valid(e)) continue;
-          float ta = 0.f, tb = 0.f;
-          for (int h = 0; h < p.team_heads; ++h) {
-            ta += sums[h * padded + c * kEach + 2 * e];
-            tb += sums[h * padded + c * kEach + 2 * e + 1];
+          if (!valid(side, e)) continue;
+          to[place_a(e)] = da[side][e];
+          to[place_b(e)] = db[side][e];
+        }
+      } else {  // the heads share their weights: summed in order here, a head's sums after the other's
+        __shared__ float sums[256 * kEach];
+        const int padded = lanes * kEach;
+        lds_barrier();
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          sums[tid * kEach + 2 * e] = valid(side, e) ? da[side][e] : 0.f;
+          sums[tid * kEach + 2 * e + 1] = valid(side, e) ? db[side][e] : 0.f;
+        }
+        lds_barrier();
+        float* to = s.part + (size_t)block * p.head_dim;
+        if (slot == 0) {
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            if (e >= in_head) continue;
+            float ta = 0.f, tb = 0.f;
+            for (int h = 0; h < p.team_heads; ++h) {
+              ta += sums[h * padded + c * kEach + 2 * e];
+              tb += sums[h * padded + c * kEach + 2 * e + 1];
+            }
+            to[place_a(e)] = ta;
+            to[place_b(e)] = tb;
           }
-          to[place_a(e)] = ta;
-          to[place_b(e)] = tb;
         }
       }
     }
@@ -1010,7 +1064,7 @@ hipError_t launch_rotary_weights(const RotaryParams& p, float* dq_weight, float*
     s.part[x] = p.side[x].part;
     s.out[x] = out[x];
     s.columns[x] = out[x] ? (row ? p.side[x].heads : 1) * p.head_dim : 0;
-    s.rows[x] = p.N == 0 ? 0 : p.batch * p.shares * (row ? 1 : p.side[x].groups);
+    s.rows[x] = p.N == 0 ? 0 : p.batch * p.shares * (row ? 1 : p.groups);
     blocks[x] = (s.columns[x] + 63) / 64;
   }
   s.blocks0 = blocks[0];

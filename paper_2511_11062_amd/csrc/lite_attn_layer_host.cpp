@@ -82,7 +82,7 @@ int log2_up(int x) {
 }
 
 struct RotaryShape {
-  int lanes_log, team_heads, threads, shares, groups[2];
+  int lanes_log, team_heads, threads, shares, groups, kinds;  // kinds of workgroups
 };
 
 RotaryShape rotary_shape(const lite_attn_rotary_desc_t& d, bool bwd) {
@@ -91,16 +91,16 @@ RotaryShape rotary_shape(const lite_attn_rotary_desc_t& d, bool bwd) {
   const int most = std::max(d.heads_q, d.heads_k), lanes = 1 << s.lanes_log;
   s.team_heads = d.norm == LITE_ATTN_NORM_ROW ? most : std::min(most, std::max(1, 256 / lanes));
   s.threads = (s.team_heads * lanes + 63) / 64 * 64;
-  s.groups[0] = (d.heads_q + s.team_heads - 1) / s.team_heads;
-  s.groups[1] = (d.heads_k + s.team_heads - 1) / s.team_heads;
-  s.shares = shares_of((int64_t)d.batch * (s.groups[0] + s.groups[1]), d.seqlen, s.threads / 64, bwd ? 16 : 24);
+  s.groups = (most + s.team_heads - 1) / s.team_heads;
+  s.kinds = s.groups * (rotary_sides(d.norm, bwd) == 1 && d.heads_k ? 2 : 1);
+  s.shares = shares_of((int64_t)d.batch * s.kinds, d.seqlen, s.threads / 64, 16);
   return s;
 }
 
 // Floats that one share leaves for the weights' gradient of a side.
 size_t rotary_part(const lite_attn_rotary_desc_t& d, const RotaryShape& s, int side) {
   const int heads = side ? d.heads_k : d.heads_q;
-  return (size_t)(d.norm == LITE_ATTN_NORM_ROW ? heads : s.groups[side]) * d.head_dim;
+  return (size_t)(d.norm == LITE_ATTN_NORM_ROW ? heads : heads ? s.groups : 0) * d.head_dim;
 }
 
 int fill_rotary(const lite_attn_rotary_desc_t& d, const lite_attn_positions_t& at, const void* const weights[2],
@@ -118,12 +118,12 @@ int fill_rotary(const lite_attn_rotary_desc_t& d, const lite_attn_positions_t& a
     if (!good_vector(weights[x], d.weight_dtype)) return LITE_ATTN_EINVAL;
     p->side[x].w = weights[x];
     p->side[x].heads = x ? d.heads_k : d.heads_q;
-    p->side[x].groups = s.groups[x];
     p->side[x].inv_count = 1.f / (float)(d.head_dim * (d.norm == LITE_ATTN_NORM_ROW ? std::max(1, p->side[x].heads) : 1));
   }
   p->freqs = at.freqs;
   p->positions = at.positions;
   p->positions_stride_b = at.positions_stride_b;
+  p->sides = d.heads_k ? 2 : 1;
   p->batch = d.batch;
   p->N = d.seqlen;
   p->shares = s.shares;
@@ -131,6 +131,7 @@ int fill_rotary(const lite_attn_rotary_desc_t& d, const lite_attn_positions_t& a
   p->pairs = d.pairs;
   p->lanes_log = s.lanes_log;
   p->team_heads = s.team_heads;
+  p->groups = s.groups;
   p->norm = d.norm;
   p->halves = d.halves;
   p->weight_dtype = d.weight_dtype;
@@ -195,7 +196,7 @@ int plan_rotary(const lite_attn_rotary_desc_t& d, const lite_attn_rotary_fwd_t& 
     set(p->side[x].xs, in, d.dtype);
     set(p->side[x].os, out, d.dtype);
   }
-  return launch_of(d.batch, (int64_t)s.shares * (s.groups[0] + s.groups[1]), s.threads, l);
+  return launch_of(d.batch, (int64_t)s.shares * s.kinds, s.threads, l);
 }
 
 int plan_rotary(const lite_attn_rotary_desc_t& d, const lite_attn_rotary_bwd_t& a, RotaryParams* p, LayerLaunch* l) {
@@ -227,7 +228,7 @@ int plan_rotary(const lite_attn_rotary_desc_t& d, const lite_attn_rotary_bwd_t& 
     if (grads[x]) p->side[x].part = part;
     part += (size_t)d.batch * s.shares * rotary_part(d, s, x);
   }
-  return launch_of(d.batch, (int64_t)s.shares * (s.groups[0] + s.groups[1]), s.threads, l);
+  return launch_of(d.batch, (int64_t)s.shares * s.kinds, s.threads, l);
 }
 
 namespace {

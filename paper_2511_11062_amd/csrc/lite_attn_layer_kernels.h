@@ -26,11 +26,15 @@ struct RotarySide {
   const void* w;      // weights or null
   float* part;        // backwards: [batch * shares][heads or groups][head_dim] sums for the weights' gradient, or null
   float inv_count;    // 1 / entries that a norm goes over
-  int heads, groups;  // groups of RotaryParams::team_heads heads
+  int heads;
 };
+
+// Of q and k, how many a workgroup takes.
+constexpr int rotary_sides(int norm, bool bwd) { return bwd && norm != LITE_ATTN_NORM_NONE ? 1 : 2; }
 
 struct RotaryParams {
   RotarySide side[2];
+  int sides;             // 2, or 1: there is no k
   const double* freqs;
   const int32_t* positions;
   int64_t positions_stride_b;
@@ -38,7 +42,8 @@ struct RotaryParams {
   int shares;            // share x of a batch entry: tokens x, x + shares, x + 2 shares, ...
   int head_dim, pairs;
   int lanes_log;         // a head takes 1 << lanes_log threads of kEach entries
-  int team_heads;        // heads that a workgroup takes
+  int team_heads;        // heads that a workgroup takes, of q and of k
+  int groups;            // of as many heads
   int norm, halves, weight_dtype;
   int token_start, area, width, video;  // area = height * width, video = frames * area
   float eps;
