@@ -586,45 +586,54 @@ __global__ __launch_bounds__(1024) void sum_rows_kernel(const RowSums p) {
 
 // ---- residual stream ---------------------------------------------------------------------------------------------------
 
-// The columns of a row that a thread holds: kEach in a row, or, of RAGGED rows (of a number of entries that kEach does not
-// divide), one of each `team`.  What lies behind the row reads as 0 and is not written.
-template <bool RAGGED>
+// The columns of a row that a thread holds: kEach in a row; four and four, where 32-bit entries are among them, so that the lanes
+// of an access of 16 bytes each lie side by side; of ragged rows (of a number of entries that kEach does not divide) one of each
+// `team`.  What lies behind the row reads as 0 and is not written.
+enum Spread { kEights, kFours, kOnes };
+template <Spread S>
 struct Columns {
   int thread, team, D;
-  __device__ __forceinline__ int at(int e) const { return RAGGED ? thread + e * team : thread * kEach + e; }
-  __device__ __forceinline__ bool has(int e) const { return RAGGED ? at(e) < D : thread * kEach < D; }
+  __device__ __forceinline__ int at(int e) const {
+    return S == kOnes ? thread + e * team : S == kFours ? (e / 4 * team + thread) * 4 + e % 4 : thread * kEach + e;
+  }
+  __device__ __forceinline__ bool has(int e) const { return at(S == kOnes ? e : S == kFours ? e / 4 * 4 : 0) < D; }
 };
-
-template <class Kind, bool RAGGED>
-constexpr int kRowStores = RAGGED ? kEach : Piece<Kind>::kSize / 2;
-template <bool RAGGED, class Kind>
-__device__ __forceinline__ void load_row(Buffer from, const Columns<RAGGED>& col, Piece<Kind>& to) {
-  if constexpr (RAGGED) {
+template <class Kind, Spread S>
+constexpr int kRowAccesses = S == kOnes ? kEach : S == kFours ? 2 : Piece<Kind>::kSize / 2;  // loads or stores of a row
+template <Spread S, class Kind>
+__device__ __forceinline__ void load_row(Buffer from, const Columns<S>& col, Piece<Kind>& to) {
+  if constexpr (S == kOnes) {
 #pragma unroll
     for (int e = 0; e < kEach; e += 2) to.load_two(e, from, col.at(e) * to.kSize, col.at(e + 1) * to.kSize);
+  } else if constexpr (S == kFours) {
+    to.load_run(0, from, col.at(0) * to.kSize);
+    to.load_run(1, from, col.at(4) * to.kSize);
   } else {
     to.load(from, col.at(0) * to.kSize);
   }
 }
-template <class Kind, bool RAGGED>
-__device__ __forceinline__ void store_row(Buffer to, const Columns<RAGGED>& col, const float* x) {
+template <class Kind, Spread S>
+__device__ __forceinline__ void store_row(Buffer to, const Columns<S>& col, const float* x) {
   Piece<Kind> out;
   out.pack(x);
-  if constexpr (RAGGED) {
+  if constexpr (S == kOnes) {
 #pragma unroll
     for (int e = 0; e < kEach; e += 2) out.store_two(e, to, col.at(e) * out.kSize, col.at(e + 1) * out.kSize);
+  } else if constexpr (S == kFours) {
+    out.store_run(0, to, col.at(0) * out.kSize);
+    out.store_run(1, to, col.at(4) * out.kSize);
   } else {
     out.store(to, col.at(0) * out.kSize);
   }
 }
-template <class Kind, bool RAGGED>
-__device__ __forceinline__ void load_vector(const char* p, const Columns<RAGGED>& col, float* to) {
+template <class Kind, Spread S>
+__device__ __forceinline__ void load_vector(const char* p, const Columns<S>& col, float* to) {
   Piece<Kind> v;
   load_row(Walk{const_cast<char*>(p), 0, col.D * v.kSize}.row(), col, v);
   v.unpack(to);
 }
-template <bool RAGGED>
-__device__ __forceinline__ void load_params(const void* p, int dtype, const Columns<RAGGED>& col, float* to, float missing) {
+template <Spread S>
+__device__ __forceinline__ void load_params(const void* p, int dtype, const Columns<S>& col, float* to, float missing) {
   if (!p) {
 #pragma unroll
     for (int e = 0; e < kEach; ++e) to[e] = missing;
@@ -637,8 +646,8 @@ __device__ __forceinline__ void load_params(const void* p, int dtype, const Colu
   }
 }
 // A row of modulation.
-template <bool RAGGED>
-__device__ __forceinline__ void load_mod(const Lines& l, int dtype, int b, int g, const Columns<RAGGED>& col, float* to,
+template <Spread S>
+__device__ __forceinline__ void load_mod(const Lines& l, int dtype, int b, int g, const Columns<S>& col, float* to,
                                          float missing) {
   load_params(l.data ? l.data + b * l.stride_b + g * l.stride_n : nullptr, dtype, col, to, missing);
 }
@@ -665,9 +674,9 @@ struct Team {
 };
 
 // Gradient through a norm: d -> rstd (d - mean(d) [LAYER] - n mean(d n)).
-template <bool RAGGED>
+template <Spread S>
 __device__ __forceinline__ void norm_back(Team& team, float* d, const float* n, float rstd, int kind, float inv_D,
-                                          const Columns<RAGGED>& col) {
+                                          const Columns<S>& col) {
   f32x2 s = {0.f, 0.f};
 #pragma unroll
   for (int e = 0; e < kEach; ++e) {
@@ -691,8 +700,8 @@ struct Counts {
 struct Stats {
   float mean, rstd;
 };
-template <bool RAGGED>
-__device__ __forceinline__ Stats row_stats(Team& team, const float* x, const Columns<RAGGED>& col, int kind, float eps, float inv_D,
+template <Spread S>
+__device__ __forceinline__ Stats row_stats(Team& team, const float* x, const Columns<S>& col, int kind, float eps, float inv_D,
                                            const Counts& counts) {
   float mean = 0.f;
   if (kind == LITE_ATTN_NORM_LAYER) {
@@ -736,8 +745,8 @@ struct Share {
   }
 };
 
-template <bool RAGGED>
-__device__ __forceinline__ Counts count_columns(const ResidualParams& p, const Columns<RAGGED>& col, float* in_waves) {
+template <Spread S>
+__device__ __forceinline__ Counts count_columns(const ResidualParams& p, const Columns<S>& col, float* in_waves) {
   float mine = 0.f;
 #pragma unroll
   for (int e = 0; e < kEach; ++e) mine += col.has(e) ? 1.f : 0.f;
@@ -748,13 +757,13 @@ __device__ __forceinline__ Counts count_columns(const ResidualParams& p, const C
   return {1.f / mine, w < (int)(blockDim.x >> 6) ? in_waves[w] : 0.f};
 }
 
-template <class KindX, class KindY, bool RAGGED>
+template <class KindX, class KindY, Spread S>
 __global__ __launch_bounds__(kMaxTeam) void residual_fwd_kernel(const ResidualParams p) {
   __shared__ WaveRoom room;
   __shared__ float in_waves[kMaxTeam / 64];
   const Share share(p);
   if (share.n0 >= share.end) return;  // (a group of fewer rows than shares)
-  const Columns<RAGGED> col = {(int)threadIdx.x, (int)blockDim.x, p.D};
+  const Columns<S> col = {(int)threadIdx.x, (int)blockDim.x, p.D};
   Team team = {blockDim.x > 64, 0, &room};
   const int row_x = p.D * Piece<KindX>::kSize, row_y = p.D * Piece<KindY>::kSize;
 
@@ -789,7 +798,7 @@ __global__ __launch_bounds__(kMaxTeam) void residual_fwd_kernel(const ResidualPa
 #pragma unroll
     for (int e = 0; e < kEach; ++e) add[e] += t[e];
   }
-  no_stores<kRowStores<KindX, RAGGED> + kRowStores<KindY, RAGGED>>(x_to);
+  no_stores<kRowAccesses<KindX, S> + kRowAccesses<KindY, S>>(x_to);
   for (int n = share.n0; n < share.end; n += share.step) {
     const Piece<KindX> px = next_x;
     const Piece<KindY> py = next_y;
@@ -828,13 +837,13 @@ __global__ __launch_bounds__(kMaxTeam) void residual_fwd_kernel(const ResidualPa
 //   dy = the same of dp post_w, dp = alpha gate dx, with n_y = post(y)
 // and over the tokens of a row of modulation A = sum dh n, S = sum dh, C = sum dx n_y, from which all six gradients of the
 // parameters follow (group_sums_kernel): three sums in registers, where each gradient by itself would need six.
-template <class KindX, class KindY, bool RAGGED>
+template <class KindX, class KindY, Spread S>
 __global__ __launch_bounds__(kMaxTeam) void residual_bwd_kernel(const ResidualParams p) {
   __shared__ WaveRoom room;
   __shared__ float in_waves[kMaxTeam / 64];
   const Share share(p);
   if (share.n0 >= share.end) return;  // (a group of fewer rows than shares)
-  const Columns<RAGGED> col = {(int)threadIdx.x, (int)blockDim.x, p.D};
+  const Columns<S> col = {(int)threadIdx.x, (int)blockDim.x, p.D};
   Team team = {blockDim.x > 64, 0, &room};
   const int row_x = p.D * Piece<KindX>::kSize, row_y = p.D * Piece<KindY>::kSize;
 
@@ -867,7 +876,7 @@ __global__ __launch_bounds__(kMaxTeam) void residual_bwd_kernel(const ResidualPa
       sum_a[e] = sum_s[e] = sum_c[e] = 0.f;
     }
   }
-  no_stores<kRowStores<KindX, RAGGED> + kRowStores<KindY, RAGGED>>(dx_to);
+  no_stores<kRowAccesses<KindX, S> + kRowAccesses<KindY, S>>(dx_to);
   for (int n = share.n0; n < share.end; n += share.step) {
     // what the row needs first is asked for a row ahead, the rest now
     const Piece<KindX> px = next_x;
@@ -1030,16 +1039,17 @@ void launch_rotary_kind(const RotaryParams& p, const LayerLaunch& l, bool bwd, h
   bwd ? launch_rotary_way<Kind, true>(p, l, st) : launch_rotary_way<Kind, false>(p, l, st);
 }
 
-template <class KindX, class KindY, bool RAGGED>
+template <class KindX, class KindY, Spread S>
 void launch_residual_way(const ResidualParams& p, const LayerLaunch& l, bool bwd, hipStream_t st) {
   if (bwd)
-    residual_bwd_kernel<KindX, KindY, RAGGED><<<l.blocks, l.threads, 0, st>>>(p);
+    residual_bwd_kernel<KindX, KindY, S><<<l.blocks, l.threads, 0, st>>>(p);
   else
-    residual_fwd_kernel<KindX, KindY, RAGGED><<<l.blocks, l.threads, 0, st>>>(p);
+    residual_fwd_kernel<KindX, KindY, S><<<l.blocks, l.threads, 0, st>>>(p);
 }
 template <class KindX, class KindY>
 void launch_residual_kind(const ResidualParams& p, const LayerLaunch& l, bool bwd, hipStream_t st) {
-  p.D % kEach ? launch_residual_way<KindX, KindY, true>(p, l, bwd, st) : launch_residual_way<KindX, KindY, false>(p, l, bwd, st);
+  constexpr Spread kWhole = Piece<KindX>::kSize == 4 ? kFours : kEights;
+  p.D % kEach ? launch_residual_way<KindX, KindY, kOnes>(p, l, bwd, st) : launch_residual_way<KindX, KindY, kWhole>(p, l, bwd, st);
 }
 
 }  // namespace
