@@ -53,6 +53,9 @@ struct F32 {
 // for a row that was asked for ahead does not wait for the stores behind it.  Offsets need the alignment of an element only.
 typedef __amdgpu_buffer_rsrc_t Buffer;
 constexpr int kBufferFlags = 0x00020000;
+// Cache policy of rows (bit 1, non-temporal): each is read or written once and makes room at once.  us without -> with, forwards
+// 32760 x 1536 (stream in 32 bits) 111 -> 104, 75600 x 5120 (bf16) 588 -> 514, rotary of 12 heads 81 -> 77, backwards 131 -> 121.
+constexpr int kStreamed = 2;
 struct Walk {
   char* at;
   int64_t stride;
@@ -83,18 +86,18 @@ struct Piece {
 
   __device__ __forceinline__ void load_run(int run, Buffer from, int offset) {
     if constexpr (kNarrow) {
-      const u32x2 v = __builtin_amdgcn_raw_buffer_load_b64(from, offset, 0, 0);
+      const u32x2 v = __builtin_amdgcn_raw_buffer_load_b64(from, offset, 0, kStreamed);
       w[2 * run] = v[0];
       w[2 * run + 1] = v[1];
     } else {
-      const u32x4 v = __builtin_amdgcn_raw_buffer_load_b128(from, offset, 0, 0);
+      const u32x4 v = __builtin_amdgcn_raw_buffer_load_b128(from, offset, 0, kStreamed);
 #pragma unroll
       for (int x = 0; x < 4; ++x) w[4 * run + x] = v[x];
     }
   }
   __device__ __forceinline__ void load(Buffer from, int offset) {
     if constexpr (kNarrow) {
-      const u32x4 v = __builtin_amdgcn_raw_buffer_load_b128(from, offset, 0, 0);
+      const u32x4 v = __builtin_amdgcn_raw_buffer_load_b128(from, offset, 0, kStreamed);
 #pragma unroll
       for (int x = 0; x < 4; ++x) w[x] = v[x];
     } else {
@@ -105,12 +108,12 @@ struct Piece {
   // Entries e and e + 1, each from a place of its own.
   __device__ __forceinline__ void load_two(int e, Buffer from, int offset0, int offset1) {
     if constexpr (kNarrow) {
-      const uint32_t lo = (uint16_t)__builtin_amdgcn_raw_buffer_load_b16(from, offset0, 0, 0);
-      const uint32_t hi = (uint16_t)__builtin_amdgcn_raw_buffer_load_b16(from, offset1, 0, 0);
+      const uint32_t lo = (uint16_t)__builtin_amdgcn_raw_buffer_load_b16(from, offset0, 0, kStreamed);
+      const uint32_t hi = (uint16_t)__builtin_amdgcn_raw_buffer_load_b16(from, offset1, 0, kStreamed);
       w[e / 2] = lo | hi << 16;
     } else {
-      w[e] = __builtin_amdgcn_raw_buffer_load_b32(from, offset0, 0, 0);
-      w[e + 1] = __builtin_amdgcn_raw_buffer_load_b32(from, offset1, 0, 0);
+      w[e] = __builtin_amdgcn_raw_buffer_load_b32(from, offset0, 0, kStreamed);
+      w[e + 1] = __builtin_amdgcn_raw_buffer_load_b32(from, offset1, 0, kStreamed);
     }
   }
   __device__ __forceinline__ void unpack(float* x) const {
@@ -138,13 +141,13 @@ struct Piece {
   }
   __device__ __forceinline__ void store_run(int run, Buffer to, int offset) const {
     if constexpr (kNarrow)
-      __builtin_amdgcn_raw_buffer_store_b64(u32x2{w[2 * run], w[2 * run + 1]}, to, offset, 0, 0);
+      __builtin_amdgcn_raw_buffer_store_b64(u32x2{w[2 * run], w[2 * run + 1]}, to, offset, 0, kStreamed);
     else
-      __builtin_amdgcn_raw_buffer_store_b128(u32x4{w[4 * run], w[4 * run + 1], w[4 * run + 2], w[4 * run + 3]}, to, offset, 0, 0);
+      __builtin_amdgcn_raw_buffer_store_b128(u32x4{w[4 * run], w[4 * run + 1], w[4 * run + 2], w[4 * run + 3]}, to, offset, 0, kStreamed);
   }
   __device__ __forceinline__ void store(Buffer to, int offset) const {
     if constexpr (kNarrow) {
-      __builtin_amdgcn_raw_buffer_store_b128(u32x4{w[0], w[1], w[2], w[3]}, to, offset, 0, 0);
+      __builtin_amdgcn_raw_buffer_store_b128(u32x4{w[0], w[1], w[2], w[3]}, to, offset, 0, kStreamed);
     } else {
       store_run(0, to, offset);
       store_run(1, to, offset + 16);
@@ -152,11 +155,11 @@ struct Piece {
   }
   __device__ __forceinline__ void store_two(int e, Buffer to, int offset0, int offset1) const {
     if constexpr (kNarrow) {
-      __builtin_amdgcn_raw_buffer_store_b16((uint16_t)w[e / 2], to, offset0, 0, 0);
-      __builtin_amdgcn_raw_buffer_store_b16((uint16_t)(w[e / 2] >> 16), to, offset1, 0, 0);
+      __builtin_amdgcn_raw_buffer_store_b16((uint16_t)w[e / 2], to, offset0, 0, kStreamed);
+      __builtin_amdgcn_raw_buffer_store_b16((uint16_t)(w[e / 2] >> 16), to, offset1, 0, kStreamed);
     } else {
-      __builtin_amdgcn_raw_buffer_store_b32(w[e], to, offset0, 0, 0);
-      __builtin_amdgcn_raw_buffer_store_b32(w[e + 1], to, offset1, 0, 0);
+      __builtin_amdgcn_raw_buffer_store_b32(w[e], to, offset0, 0, kStreamed);
+      __builtin_amdgcn_raw_buffer_store_b32(w[e + 1], to, offset1, 0, kStreamed);
     }
   }
 };

@@ -61,11 +61,17 @@ bool good_vector(const T* p, int dtype) {
 }
 bool good_grad(const float* p) { return ((uintptr_t)p & 3) == 0; }
 
-// Shares that each of `kinds` kinds of rows is dealt to (at most `rows`, of a kind), in workgroups of `waves` waves, `per_cu`
-// waves on a CU altogether.
-int shares_of(int64_t kinds, int rows, int waves, int per_cu) {
-  const int64_t side_by_side = (int64_t)kCUs * std::max(1, (per_cu + waves / 2) / waves);
-  return (int)std::max<int64_t>(1, std::min<int64_t>(rows, side_by_side / kinds));
+// Shares that each of `kinds` kinds of rows is dealt to, at most `rows` (of a kind).  A workgroup of `waves` waves has a row of
+// `bytes` asked for at any time.  Memory gives most when 18 KB are asked for on each CU, in whole workgroups for each CU; more
+// of them get into each other's way.  us at 256 / 512 / 768 / 1024 / 1280 / 1536 workgroups: forwards 32760 x 1536, 9 KB a row,
+// 114 / 104 / 111 / 111 / 113 / 114, backwards, 18 KB, 159 / 167 / 185 / 188 / 199 / 199, 75600 x 5120, 20 KB, 514 / 564 / 555 / 592
+// / 614 / 607, rotary of 12 heads, 3 KB, 167 / 109 / 87 / 82 / 77 / 79, backwards, 6 KB, 220 / 140 / 121 / 121 / 121 / 123.  Kinds
+// that do not go evenly into that are dealt to four times as many, to be taken as CUs get free.
+int shares_of(int64_t kinds, int rows, int waves, int64_t bytes) {
+  const int64_t per_cu = std::max<int64_t>(1, std::min<int64_t>((18432 + bytes - 1) / bytes, 32 / waves));
+  const int64_t side_by_side = kCUs * per_cu;
+  const int64_t shares = kinds * 4 <= side_by_side ? side_by_side / kinds : (4 * side_by_side + kinds - 1) / kinds;
+  return (int)std::max<int64_t>(1, std::min<int64_t>(rows, shares));
 }
 
 int launch_of(int64_t kinds, int64_t shares, int threads, LayerLaunch* l) {
@@ -93,7 +99,9 @@ RotaryShape rotary_shape(const lite_attn_rotary_desc_t& d, bool bwd) {
   s.threads = (s.team_heads * lanes + 63) / 64 * 64;
   s.groups = (most + s.team_heads - 1) / s.team_heads;
   s.kinds = s.groups * (rotary_sides(d.norm, bwd) == 1 && d.heads_k ? 2 : 1);
-  s.shares = shares_of((int64_t)d.batch * s.kinds, d.seqlen, s.threads / 64, 16);
+  const int64_t row = (int64_t)s.team_heads * d.head_dim * size_of(d.dtype);
+  s.shares = shares_of((int64_t)d.batch * s.kinds, d.seqlen, s.threads / 64,
+                       bwd && d.norm != LITE_ATTN_NORM_NONE ? 2 * row : row);
   return s;
 }
 
@@ -246,7 +254,7 @@ ResidualShape residual_shape(const lite_attn_residual_desc_t& d, bool bwd) {
   ResidualShape s;
   s.threads = (d.dim + 64 * kEach - 1) / (64 * kEach) * 64;
   s.shares = shares_of(std::max<int64_t>(1, (int64_t)d.batch * groups_of(d)), std::min(d.tokens_per_mod, d.seqlen),
-                       s.threads / 64, bwd ? 16 : 24);
+                       s.threads / 64, (int64_t)d.dim * (size_of(d.dtype) + size_of(d.stream_dtype)) * (bwd ? 2 : 1));
   return s;
 }
 
