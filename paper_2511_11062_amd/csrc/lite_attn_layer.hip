@@ -224,6 +224,18 @@ __device__ __forceinline__ f32x2 get_waves(const WaveRoom* room, int turn) {
 
 // ---- rotary positions --------------------------------------------------------------------------------------------------
 
+// Brings a kernel's arguments into the scalar cache, all lines of 64 bytes at once: they come from host memory, and left to the
+// places of their first use a workgroup would wait for one line after the other.
+template <int kBytes>
+__device__ __forceinline__ void touch_arguments() {
+  typedef const __attribute__((address_space(4))) uint32_t* Words;
+  const Words a = (Words)__builtin_amdgcn_kernarg_segment_ptr();
+  uint32_t x = 0;
+#pragma unroll
+  for (int line = 0; line < (kBytes + 63) / 64; ++line) x |= a[min(16 * line, kBytes / 4 - 1)];
+  asm volatile("" ::"s"(x));
+}
+
 // Where a token stands.
 struct Position {
   int at[3];
@@ -257,13 +269,13 @@ __device__ __forceinline__ f32x2 angle_of(const Speed& v, const Position& at) {
 }
 
 // The angles of `count` tokens n, n + step, ..., 1 << pairs_log for each.  If those are whole waves, a wave takes a token, whose
-// position it finds by scalar instructions, and a thread keeps its pair.
-__device__ __forceinline__ void make_angles(const RotaryParams& p, const int32_t* positions, int n, int step, int count,
-                                            int pairs_log, f32x2* angles) {
+// position it finds by scalar instructions, and a thread keeps its pair (`mine`: how fast pair threadIdx.x % 64 turns).
+__device__ __forceinline__ void make_angles(const RotaryParams& p, const int32_t* positions, const Speed& mine, int n, int step,
+                                            int count, int pairs_log, f32x2* angles) {
   if (pairs_log >= 6) {
     const int waves = blockDim.x >> 6, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
     for (int first = 0; first < 1 << pairs_log; first += 64) {
-      const Speed v = speed_of(p, first + lane);
+      const Speed v = first == 0 ? mine : speed_of(p, first + lane);
       for (int x = wave; x < count; x += waves)
         angles[(x << pairs_log) + first + lane] = angle_of(v, position_of(p, positions, n + x * step));
     }
@@ -283,6 +295,7 @@ __global__ __launch_bounds__(NORM == LITE_ATTN_NORM_ROW ? kMaxTeam : 256) void r
   constexpr int kSize = Piece<Kind>::kSize;
   constexpr bool kNormed = NORM != LITE_ATTN_NORM_NONE;
   constexpr int kSides = rotary_sides(NORM, BWD);
+  touch_arguments<sizeof(RotaryParams)>();
   __shared__ f32x2 angles[kAngles];
   __shared__ WaveRoom room;
   const int tid = threadIdx.x;
@@ -340,7 +353,7 @@ __global__ __launch_bounds__(NORM == LITE_ATTN_NORM_ROW ? kMaxTeam : 256) void r
       }
     }
   };
-  auto unpack = [&](const Piece<Kind>& from, float* a, float* b) {
+  auto unpack = [&](const auto& from, float* a, float* b) {
     float x[kEach];
     from.unpack(x);
 #pragma unroll
@@ -389,22 +402,43 @@ __global__ __launch_bounds__(NORM == LITE_ATTN_NORM_ROW ? kMaxTeam : 256) void r
     if constexpr (BWD) fetch(side, in_g[side], there, next_g);
   };
   fetch_next(0, true);
+  const Speed mine = speed_of(p, tid & 63);      // (asked for before anything is waited for)
   float wa[kSides][4], wb[kSides][4], da[kSides][4], db[kSides][4];  // weights and, backwards, the sums for their gradient
   if constexpr (kNormed) {
+    auto load_weights = [&](auto kind) {
+      typedef Piece<decltype(kind)> Weights;
+      Weights v[kSides];
 #pragma unroll
-    for (int side = 0; side < kSides; ++side) {
-      const void* w = sides[side].w;
+      for (int side = 0; side < kSides; ++side) {
+        const int heads = NORM == LITE_ATTN_NORM_ROW ? sides[side].heads : 1;
+        const int bytes = sides[side].w ? heads * p.head_dim * Weights::kSize : 0;
+        const Buffer from = Walk{(char*)sides[side].w, 0, bytes}.row();
+        const int row = NORM == LITE_ATTN_NORM_ROW ? head * p.head_dim : 0;
 #pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        wa[side][e] = wb[side][e] = 1.f;
-        da[side][e] = db[side][e] = 0.f;
-        if (w && valid(side, e)) {
-          const int row = NORM == LITE_ATTN_NORM_ROW ? head * p.head_dim : 0;
-          wa[side][e] = load_param(w, p.weight_dtype, row + place_a(e));
-          wb[side][e] = load_param(w, p.weight_dtype, row + place_b(e));
+        for (int e = 0; e < kEach && !WHOLE; e += 2)
+          v[side].load_two(e, from, valid(side, e / 2) ? (row + place_a(e / 2)) * Weights::kSize : bytes,
+                           valid(side, e / 2) ? (row + place_b(e / 2)) * Weights::kSize : bytes);
+        if constexpr (WHOLE) {
+          v[side].load_run(0, from, valid(side, 0) ? (row + first) * Weights::kSize : bytes);
+          v[side].load_run(1, from, valid(side, 0) ? (row + second) * Weights::kSize : bytes);
         }
       }
-    }
+#pragma unroll
+      for (int side = 0; side < kSides; ++side) {
+        unpack(v[side], wa[side], wb[side]);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          if (!sides[side].w) wa[side][e] = wb[side][e] = 1.f;
+          da[side][e] = db[side][e] = 0.f;
+        }
+      }
+    };
+    if (p.weight_dtype == LITE_ATTN_F32)
+      load_weights(F32());
+    else if (p.weight_dtype == LITE_ATTN_BF16)
+      load_weights(Bf16());
+    else
+      load_weights(F16());
   }
   int turn = 0;
   float ca[4], sa[4];
@@ -498,7 +532,7 @@ __global__ __launch_bounds__(NORM == LITE_ATTN_NORM_ROW ? kMaxTeam : 256) void r
     if (made == 0) {
       if (n != n0) lds_barrier();
       made = min(some, (p.N - 1 - n) / step + 1);
-      make_angles(p, positions, n, step, made, pairs_log, angles);
+      make_angles(p, positions, mine, n, step, made, pairs_log, angles);
       at = 4 * c;
       lds_barrier();
     }
@@ -764,6 +798,7 @@ template <class KindX, class KindY, Spread S>
 __global__ __launch_bounds__(kMaxTeam) void residual_fwd_kernel(const ResidualParams p) {
   __shared__ WaveRoom room;
   __shared__ float in_waves[kMaxTeam / 64];
+  touch_arguments<sizeof(ResidualParams)>();
   const Share share(p);
   if (share.n0 >= share.end) return;  // (a group of fewer rows than shares)
   const Columns<S> col = {(int)threadIdx.x, (int)blockDim.x, p.D};
@@ -844,6 +879,7 @@ template <class KindX, class KindY, Spread S>
 __global__ __launch_bounds__(kMaxTeam) void residual_bwd_kernel(const ResidualParams p) {
   __shared__ WaveRoom room;
   __shared__ float in_waves[kMaxTeam / 64];
+  touch_arguments<sizeof(ResidualParams)>();
   const Share share(p);
   if (share.n0 >= share.end) return;  // (a group of fewer rows than shares)
   const Columns<S> col = {(int)threadIdx.x, (int)blockDim.x, p.D};

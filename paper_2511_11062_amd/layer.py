@@ -9,6 +9,7 @@ integer value of a hipStream_t.
 from __future__ import annotations
 
 import ctypes
+import struct
 
 import numpy as np
 
@@ -34,32 +35,6 @@ class RotaryDesc(ctypes.Structure):
     ]
 
 
-class Heads(ctypes.Structure):
-    """lite_attn_heads_t"""
-    _fields_ = [("data", ctypes.c_void_p), ("stride_b", ctypes.c_int64), ("stride_h", ctypes.c_int64),
-                ("stride_n", ctypes.c_int64)]
-
-
-class Positions(ctypes.Structure):
-    """lite_attn_positions_t"""
-    _fields_ = [("freqs", ctypes.c_void_p), ("positions", ctypes.c_void_p), ("positions_stride_b", ctypes.c_int64),
-                ("token_start", ctypes.c_int32)]
-
-
-class RotaryFwd(ctypes.Structure):
-    """lite_attn_rotary_fwd_t"""
-    _fields_ = [("q", Heads), ("k", Heads), ("q_out", Heads), ("k_out", Heads), ("q_weight", ctypes.c_void_p),
-                ("k_weight", ctypes.c_void_p), ("at", Positions)]
-
-
-class RotaryBwd(ctypes.Structure):
-    """lite_attn_rotary_bwd_t"""
-    _fields_ = [("q", Heads), ("k", Heads), ("dq_out", Heads), ("dk_out", Heads), ("dq", Heads), ("dk", Heads),
-                ("q_weight", ctypes.c_void_p), ("k_weight", ctypes.c_void_p), ("at", Positions),
-                ("dq_weight", ctypes.c_void_p), ("dk_weight", ctypes.c_void_p), ("workspace", ctypes.c_void_p),
-                ("workspace_bytes", ctypes.c_size_t)]
-
-
 class ResidualDesc(ctypes.Structure):
     """lite_attn_residual_desc_t"""
     _fields_ = [
@@ -70,31 +45,20 @@ class ResidualDesc(ctypes.Structure):
     ]
 
 
-class Rows(ctypes.Structure):
-    """lite_attn_rows_t"""
-    _fields_ = [("data", ctypes.c_void_p), ("stride_b", ctypes.c_int64), ("stride_n", ctypes.c_int64)]
+# The argument structs, packed for each call (a third of the time that filling a ctypes.Structure takes): P an address, q a
+# stride, four of a lite_attn_heads_t, three of a lite_attn_rows_t.
+_POSITIONS = "PPqi0P"                                                  # lite_attn_positions_t
+_ROTARY_FWD = struct.Struct("@" + 4 * "Pqqq" + "PP" + _POSITIONS)      # lite_attn_rotary_fwd_t
+_ROTARY_BWD = struct.Struct("@" + 6 * "Pqqq" + "PP" + _POSITIONS + "PPPN")  # lite_attn_rotary_bwd_t
+_RESIDUAL_FWD = struct.Struct("@" + 7 * "Pqq" + "PPP")                 # lite_attn_residual_fwd_t
+_RESIDUAL_BWD = struct.Struct("@" + 8 * "Pqq" + "PPP" + 6 * "P" + "PN")  # lite_attn_residual_bwd_t
+_NO_HEADS = (0, 0, 0, 0)
+_NO_ROWS = (0, 0, 0)
 
-
-class ResidualFwd(ctypes.Structure):
-    """lite_attn_residual_fwd_t"""
-    _fields_ = [("x", Rows), ("y", Rows), ("x_out", Rows), ("h", Rows), ("gate", Rows), ("scale", Rows), ("shift", Rows),
-                ("post_weight", ctypes.c_void_p), ("pre_weight", ctypes.c_void_p), ("pre_bias", ctypes.c_void_p)]
-
-
-class ResidualBwd(ctypes.Structure):
-    """lite_attn_residual_bwd_t"""
-    _fields_ = [("dh", Rows), ("dx_out", Rows), ("x_out", Rows), ("y", Rows), ("dx", Rows), ("dy", Rows), ("gate", Rows),
-                ("scale", Rows), ("post_weight", ctypes.c_void_p), ("pre_weight", ctypes.c_void_p),
-                ("pre_bias", ctypes.c_void_p), ("dgate", ctypes.c_void_p), ("dscale", ctypes.c_void_p),
-                ("dshift", ctypes.c_void_p), ("dpost_weight", ctypes.c_void_p), ("dpre_weight", ctypes.c_void_p),
-                ("dpre_bias", ctypes.c_void_p), ("workspace", ctypes.c_void_p), ("workspace_bytes", ctypes.c_size_t)]
-
-
-for _n, _desc, _args in (("rotary_fwd", RotaryDesc, RotaryFwd), ("rotary_bwd", RotaryDesc, RotaryBwd),
-                         ("residual_norm_fwd", ResidualDesc, ResidualFwd),
-                         ("residual_norm_bwd", ResidualDesc, ResidualBwd)):
+for _n, _desc in (("rotary_fwd", RotaryDesc), ("rotary_bwd", RotaryDesc), ("residual_norm_fwd", ResidualDesc),
+                  ("residual_norm_bwd", ResidualDesc)):
     _f = getattr(_lib, "lite_attn_" + _n)
-    _f.argtypes = [ctypes.POINTER(_desc), ctypes.POINTER(_args), ctypes.c_void_p]
+    _f.argtypes = [ctypes.POINTER(_desc), ctypes.c_char_p, ctypes.c_void_p]
     _f.restype = ctypes.c_int
 for _n, _desc in (("rotary_bwd_workspace", RotaryDesc), ("residual_norm_bwd_workspace", ResidualDesc)):
     _f = getattr(_lib, "lite_attn_" + _n)
@@ -114,16 +78,16 @@ def make_rotary_desc(batch, seqlen, heads_q, heads_k, head_dim=128, *, dtype=LIT
 def lite_attn_rotary_fwd(desc, q, k, q_out, k_out, freqs, *, q_weight=0, k_weight=0, positions=0, positions_stride_b=0,
                          token_start=0, hip_stream):
     _check(_lib.lite_attn_rotary_fwd(
-        desc, RotaryFwd(q or (), k or (), q_out or (), k_out or (), q_weight, k_weight,
-                        (freqs, positions, positions_stride_b, token_start)), hip_stream))
+        desc, _ROTARY_FWD.pack(*(q or _NO_HEADS), *(k or _NO_HEADS), *(q_out or _NO_HEADS), *(k_out or _NO_HEADS), q_weight,
+                               k_weight, freqs, positions, positions_stride_b, token_start), hip_stream))
 
 
 def lite_attn_rotary_bwd(desc, q, k, dq_out, dk_out, dq, dk, freqs, *, q_weight=0, k_weight=0, dq_weight=0, dk_weight=0,
                          workspace=0, workspace_bytes=0, positions=0, positions_stride_b=0, token_start=0, hip_stream):
     _check(_lib.lite_attn_rotary_bwd(
-        desc, RotaryBwd(q or (), k or (), dq_out or (), dk_out or (), dq or (), dk or (), q_weight, k_weight,
-                        (freqs, positions, positions_stride_b, token_start), dq_weight, dk_weight, workspace,
-                        workspace_bytes), hip_stream))
+        desc, _ROTARY_BWD.pack(*(q or _NO_HEADS), *(k or _NO_HEADS), *(dq_out or _NO_HEADS), *(dk_out or _NO_HEADS),
+                               *(dq or _NO_HEADS), *(dk or _NO_HEADS), q_weight, k_weight, freqs, positions,
+                               positions_stride_b, token_start, dq_weight, dk_weight, workspace, workspace_bytes), hip_stream))
 
 
 def lite_attn_rotary_bwd_workspace(desc: RotaryDesc) -> int:
@@ -149,17 +113,19 @@ def make_residual_desc(batch, seqlen, dim, *, dtype=LITE_ATTN_BF16, stream_dtype
 def lite_attn_residual_norm_fwd(desc, x, y, x_out, h, *, gate=None, scale=None, shift=None, post_weight=0, pre_weight=0,
                                 pre_bias=0, hip_stream):
     _check(_lib.lite_attn_residual_norm_fwd(
-        desc, ResidualFwd(x or (), y or (), x_out or (), h or (), gate or (), scale or (), shift or (), post_weight, pre_weight,
-                          pre_bias), hip_stream))
+        desc, _RESIDUAL_FWD.pack(*(x or _NO_ROWS), *(y or _NO_ROWS), *(x_out or _NO_ROWS), *(h or _NO_ROWS),
+                                 *(gate or _NO_ROWS), *(scale or _NO_ROWS), *(shift or _NO_ROWS), post_weight, pre_weight,
+                                 pre_bias), hip_stream))
 
 
 def lite_attn_residual_norm_bwd(desc, dh, dx_out, x_out, y, dx, dy, *, gate=None, scale=None, post_weight=0, pre_weight=0,
                                 pre_bias=0, dgate=0, dscale=0, dshift=0, dpost_weight=0, dpre_weight=0, dpre_bias=0,
                                 workspace=0, workspace_bytes=0, hip_stream):
     _check(_lib.lite_attn_residual_norm_bwd(
-        desc, ResidualBwd(dh or (), dx_out or (), x_out or (), y or (), dx or (), dy or (), gate or (), scale or (),
-                          post_weight, pre_weight, pre_bias, dgate, dscale, dshift, dpost_weight, dpre_weight, dpre_bias,
-                          workspace, workspace_bytes), hip_stream))
+        desc, _RESIDUAL_BWD.pack(*(dh or _NO_ROWS), *(dx_out or _NO_ROWS), *(x_out or _NO_ROWS), *(y or _NO_ROWS),
+                                 *(dx or _NO_ROWS), *(dy or _NO_ROWS), *(gate or _NO_ROWS), *(scale or _NO_ROWS), post_weight,
+                                 pre_weight, pre_bias, dgate, dscale, dshift, dpost_weight, dpre_weight, dpre_bias, workspace,
+                                 workspace_bytes), hip_stream))
 
 
 def lite_attn_residual_norm_bwd_workspace(desc: ResidualDesc) -> int:
