@@ -42,8 +42,8 @@ extern "C" {
 typedef struct {
   int32_t batch, seqlen;    /* tokens of the call (>= 0: nothing to do), of each batch entry */
   int32_t heads_q, heads_k; /* heads of q, >= 1, and of k, >= 0: 0 = the call has no k */
-  int32_t head_dim;         /* even, at most 512; under NORM_ROW max(heads_q, heads_k) times head_dim rounded up to a power
-                               of two of at least 8 is at most 8192 (LITE_ATTN_EUNSUPPORTED otherwise) */
+  int32_t head_dim;         /* even, at most 512; under NORM_ROW max(heads_q, heads_k) times head_dim rounded up to a multiple
+                               of 8 is at most 8192 (LITE_ATTN_EUNSUPPORTED otherwise) */
   int32_t dtype;            /* of q, k, the results and their gradients */
   int32_t weight_dtype;     /* of q_weight and k_weight */
   int32_t norm;             /* LITE_ATTN_NORM_NONE, _HEAD or _ROW */
@@ -54,8 +54,8 @@ typedef struct {
 } lite_attn_rotary_desc_t;
 
 /* One of the tensors [batch, heads, seqlen, head_dim], head_dim contiguous, strides in elements and >= 0: results must not
-   have two elements in one place, inputs may (stride 0).  `data` has the alignment of its type.  Heads next to each other in 512 entries (four of 128)
-   lie within 2 GiB (LITE_ATTN_EUNSUPPORTED otherwise). */
+   have two elements in one place, inputs may (stride 0).  `data` has the alignment of its type.  As many heads as
+   fill 512 entries (four of 128) and one more lie within 4 GiB (LITE_ATTN_EUNSUPPORTED otherwise). */
 typedef struct {
   void* data;
   int64_t stride_b, stride_h, stride_n;

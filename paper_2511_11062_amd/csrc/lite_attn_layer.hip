@@ -189,14 +189,14 @@ __device__ __forceinline__ float sum16(float x) {
   return add_dpp<kMirror>(add_dpp<kHalfMirror>(add_dpp<kXor2>(add_dpp<kXor1>(x))));
 }
 __device__ __forceinline__ float sum64(float x) { return add_halves(add_row_pairs(sum16(x))); }
-// Sum over 1 << lanes_log neighbouring lanes, in all of them.
-__device__ __forceinline__ float sum_lanes(float x, int lanes_log) {
-  if (lanes_log >= 1) x = add_dpp<kXor1>(x);
-  if (lanes_log >= 2) x = add_dpp<kXor2>(x);
-  if (lanes_log >= 3) x = add_dpp<kHalfMirror>(x);
-  if (lanes_log >= 4) x = add_dpp<kMirror>(x);
-  if (lanes_log >= 5) x = add_row_pairs(x);
-  if (lanes_log >= 6) x = add_halves(x);
+// Sum over 1 << log neighbouring lanes, in all of them.
+__device__ __forceinline__ float sum_lanes(float x, int log) {
+  if (log >= 1) x = add_dpp<kXor1>(x);
+  if (log >= 2) x = add_dpp<kXor2>(x);
+  if (log >= 3) x = add_dpp<kHalfMirror>(x);
+  if (log >= 4) x = add_dpp<kMirror>(x);
+  if (log >= 5) x = add_row_pairs(x);
+  if (log >= 6) x = add_halves(x);
   return x;
 }
 
@@ -268,25 +268,33 @@ __device__ __forceinline__ f32x2 angle_of(const Speed& v, const Position& at) {
   return f32x2{c, s};
 }
 
-// The angles of `count` tokens n, n + step, ..., 1 << pairs_log for each.  If those are whole waves, a wave takes a token, whose
-// position it finds by scalar instructions, and a thread keeps its pair (`mine`: how fast pair threadIdx.x % 64 turns).
+// The angles of `tiles` tiles of tokens, the first of them at token n, `step` tokens from one to the next: 4 * lanes for each
+// token.  If those are whole waves, a wave takes a token, whose position it finds by scalar instructions, and a thread keeps its
+// pair (`mine`: how fast pair threadIdx.x % 64 turns).
 __device__ __forceinline__ void make_angles(const RotaryParams& p, const int32_t* positions, const Speed& mine, int n, int step,
-                                            int count, int pairs_log, f32x2* angles) {
-  if (pairs_log >= 6) {
+                                            int tiles, f32x2* angles) {
+  const int each = 4 * p.lanes, tokens = tiles * p.tokens;
+  auto token = [&](int x) {  // (of the last tile some may be none)
+    const int tile = quotient(x, p.tokens, p.per_tokens);
+    return min(p.N - 1, n + tile * step + (x - tile * p.tokens));
+  };
+  if (each % 64 == 0) {
     const int waves = blockDim.x >> 6, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
-    for (int first = 0; first < 1 << pairs_log; first += 64) {
+    for (int first = 0; first < each; first += 64) {
       const Speed v = first == 0 ? mine : speed_of(p, first + lane);
-      for (int x = wave; x < count; x += waves)
-        angles[(x << pairs_log) + first + lane] = angle_of(v, position_of(p, positions, n + x * step));
+      for (int x = wave; x < tokens; x += waves)
+        angles[x * each + first + lane] = angle_of(v, position_of(p, positions, token(x)));
     }
   } else {
-    for (int x = threadIdx.x; x < count << pairs_log; x += blockDim.x)
-      angles[x] = angle_of(speed_of(p, x & ((1 << pairs_log) - 1)), position_of(p, positions, n + (x >> pairs_log) * step));
+    for (int x = threadIdx.x; x < tokens * each; x += blockDim.x) {
+      const int t = quotient(x, each, p.per_angles);
+      angles[x] = angle_of(speed_of(p, x - t * each), position_of(p, positions, token(t)));
+    }
   }
 }
 
 // A workgroup: some heads (under NORM_ROW all) of q and the same heads of k, whose angles are the same, for a share of the
-// tokens.  A row is a token's heads of q or of k, one after the other.  (Backwards through a norm, where weights and the sums
+// tokens, one or some at a time.  A row is a token's heads of q or of k, one after the other.  (Backwards through a norm, where weights and the sums
 // for their gradient would need 32 registers, a workgroup takes q or k.)  A thread holds four pairs of a head, a[4] and b[4].
 // WHOLE: they are eight entries in a row or, of turned halves, four and four; otherwise (a head's ragged end, four pairs across
 // the end of the turned halves) every entry is fetched by itself.
@@ -298,17 +306,18 @@ __global__ __launch_bounds__(NORM == LITE_ATTN_NORM_ROW ? kMaxTeam : 256) void r
   touch_arguments<sizeof(RotaryParams)>();
   __shared__ f32x2 angles[kAngles];
   __shared__ WaveRoom room;
+  __shared__ f32x2 lane_sums[2][NORM == LITE_ATTN_NORM_HEAD ? 256 + 64 : 1];  // (threads of no head read on behind 256)
   const int tid = threadIdx.x;
   const int block = kSides == 2 ? (int)blockIdx.x : (int)blockIdx.x / p.sides;
   const RotarySide* const sides = p.side + (kSides == 2 ? 0 : (int)blockIdx.x - block * p.sides);
   const int share = block / p.groups, group = block - share * p.groups;
-  const int batch = share / p.shares, n0 = share - batch * p.shares, step = p.shares;
+  const int batch = share / p.shares, n0 = (share - batch * p.shares) * p.tokens, step = p.shares * p.tokens;
 
-  const int lanes = 1 << p.lanes_log;
-  const int slot = tid >> p.lanes_log, c = tid & (lanes - 1);
+  const int sub = quotient(tid, p.row_lanes, p.per_row), in_row = tid - sub * p.row_lanes;  // token of the tile
+  const int slot = quotient(in_row, p.lanes, p.per_lanes), c = in_row - slot * p.lanes;
   const int head = group * p.team_heads + slot;
   // pairs of the head from this thread's first on
-  const int in_head = slot < p.team_heads ? min(4, p.head_dim / 2 - 4 * c) : 0;
+  const int in_head = sub < p.tokens && slot < p.team_heads ? min(4, p.head_dim / 2 - 4 * c) : 0;
   auto valid = [&](int side, int e) { return head < sides[side].heads && (WHOLE ? in_head > 0 : e < in_head); };
   // places in the head of a[e] and b[e]
   const int P = p.pairs;
@@ -320,8 +329,10 @@ __global__ __launch_bounds__(NORM == LITE_ATTN_NORM_ROW ? kMaxTeam : 256) void r
   const bool apart = HALVES && 4 * c < P;
   const int first = place_a(0), second = apart ? first + P : first + 4;
 
-  // A wave's rows start at its first head; its other heads are `stride_h` apart.  Entries that are not there lie behind all.
-  const int wave_slot = __builtin_amdgcn_readfirstlane(slot), wave_head = group * p.team_heads + wave_slot;
+  // A wave's rows start at its first head (at the workgroup's, if that takes some tokens); other heads are `stride_h` and other
+  // tokens `stride_n` apart.  Entries that are not there lie behind all.
+  const int wave_slot = p.tokens > 1 ? 0 : __builtin_amdgcn_readfirstlane(slot);
+  const int wave_head = group * p.team_heads + wave_slot;
   struct Tensor {
     Walk walk;
     int first, second;
@@ -329,26 +340,26 @@ __global__ __launch_bounds__(NORM == LITE_ATTN_NORM_ROW ? kMaxTeam : 256) void r
   auto tensor = [&](int side, const char* data, const int64_t* s) {
     Tensor t;
     const int heads = sides[side].heads;
-    const int span = heads == 0 ? 0 : (int)(min(63 >> p.lanes_log, heads - 1) * s[1]) + p.head_dim * kSize;
-    t.walk = Walk{const_cast<char*>(data) + batch * s[0] + n0 * s[2] + wave_head * s[1], step * s[2], span};
-    const int at = (slot - wave_slot) * (int)s[1];
-    t.first = valid(side, 0) ? at + first * kSize : span;
-    t.second = valid(side, 0) ? at + second * kSize : span;
+    const int64_t span = heads == 0 ? 0 : (min(p.near_heads, heads) - 1) * s[1] + (p.tokens - 1) * s[2] + p.head_dim * kSize;
+    t.walk = Walk{const_cast<char*>(data) + batch * s[0] + n0 * s[2] + wave_head * s[1], step * s[2], (int)span};
+    const int64_t at = (slot - wave_slot) * s[1] + sub * s[2];
+    t.first = valid(side, 0) ? (int)(at + first * kSize) : (int)span;
+    t.second = valid(side, 0) ? (int)(at + second * kSize) : (int)span;
     return t;
   };
   auto fetch = [&](int side, Tensor& t, bool there, Piece<Kind>& to) {
-    const Buffer from = t.walk.row_if(there);
+    const Buffer from = t.walk.row();
     t.walk.step();
     if constexpr (WHOLE && HALVES) {
-      to.load_run(0, from, t.first);
-      to.load_run(1, from, t.second);
+      to.load_run(0, from, there ? t.first : t.walk.bytes);
+      to.load_run(1, from, there ? t.second : t.walk.bytes);
     } else if constexpr (WHOLE) {
-      to.load(from, t.first);
+      to.load(from, there ? t.first : t.walk.bytes);
     } else {
 #pragma unroll
       for (int e = 0; e < 4; ++e) {
-        const int a = valid(side, e) ? t.first + (place_a(e) - first) * kSize : t.walk.bytes;
-        const int b = valid(side, e) ? t.first + (place_b(e) - first) * kSize : t.walk.bytes;
+        const int a = there && valid(side, e) ? t.first + (place_a(e) - first) * kSize : t.walk.bytes;
+        const int b = there && valid(side, e) ? t.first + (place_b(e) - first) * kSize : t.walk.bytes;
         to.load_two(2 * e, from, a, b);
       }
     }
@@ -362,7 +373,7 @@ __global__ __launch_bounds__(NORM == LITE_ATTN_NORM_ROW ? kMaxTeam : 256) void r
       b[e] = WHOLE && HALVES && apart ? x[4 + e] : x[2 * e + 1];
     }
   };
-  auto store = [&](int side, Tensor& t, const float* ra, const float* rb) {
+  auto store = [&](int side, Tensor& t, bool there, const float* ra, const float* rb) {
     const Buffer to = t.walk.row();
     t.walk.step();
     float x[kEach];
@@ -374,15 +385,15 @@ __global__ __launch_bounds__(NORM == LITE_ATTN_NORM_ROW ? kMaxTeam : 256) void r
     Piece<Kind> out;
     out.pack(x);
     if constexpr (WHOLE && HALVES) {
-      out.store_run(0, to, t.first);
-      out.store_run(1, to, t.second);
+      out.store_run(0, to, there ? t.first : t.walk.bytes);
+      out.store_run(1, to, there ? t.second : t.walk.bytes);
     } else if constexpr (WHOLE) {
-      out.store(to, t.first);
+      out.store(to, there ? t.first : t.walk.bytes);
     } else {
 #pragma unroll
       for (int e = 0; e < 4; ++e) {
-        const int a = valid(side, e) ? t.first + (place_a(e) - first) * kSize : t.walk.bytes;
-        const int b = valid(side, e) ? t.first + (place_b(e) - first) * kSize : t.walk.bytes;
+        const int a = there && valid(side, e) ? t.first + (place_a(e) - first) * kSize : t.walk.bytes;
+        const int b = there && valid(side, e) ? t.first + (place_b(e) - first) * kSize : t.walk.bytes;
         out.store_two(2 * e, to, a, b);
       }
     }
@@ -401,7 +412,7 @@ __global__ __launch_bounds__(NORM == LITE_ATTN_NORM_ROW ? kMaxTeam : 256) void r
     if constexpr (!BWD || kNormed) fetch(side, in_x[side], there, next_x);
     if constexpr (BWD) fetch(side, in_g[side], there, next_g);
   };
-  fetch_next(0, true);
+  fetch_next(0, n0 + sub < p.N);
   const Speed mine = speed_of(p, tid & 63);      // (asked for before anything is waited for)
   float wa[kSides][4], wb[kSides][4], da[kSides][4], db[kSides][4];  // weights and, backwards, the sums for their gradient
   if constexpr (kNormed) {
@@ -442,8 +453,34 @@ __global__ __launch_bounds__(NORM == LITE_ATTN_NORM_ROW ? kMaxTeam : 256) void r
   }
   int turn = 0;
   float ca[4], sa[4];
+  // Sums over what a norm goes over: neighbouring lanes, a power of two of them; all waves; or the lanes of a head, of which each
+  // adds up all from LDS.
+  auto row_sum = [&](f32x2 x) {
+    if (p.sum_log >= 0) {
+      x[0] = sum_lanes(x[0], p.sum_log);
+      if constexpr (BWD) x[1] = sum_lanes(x[1], p.sum_log);
+      return x;
+    }
+    if constexpr (NORM == LITE_ATTN_NORM_ROW) {
+      x[0] = sum64(x[0]);
+      if constexpr (BWD) x[1] = sum64(x[1]);
+      put_waves(&room, turn, x);
+      lds_barrier();
+      x = get_waves(&room, turn);
+      x[0] = sum16(x[0]);
+      if constexpr (BWD) x[1] = sum16(x[1]);
+    } else {
+      lane_sums[turn][tid] = x;
+      lds_barrier();
+      const f32x2* const mine = &lane_sums[turn][tid - c];
+      x = mine[0];
+      for (int l = 1; l < p.lanes; ++l) x += mine[l];
+    }
+    turn ^= 1;
+    return x;
+  };
   // A row; the next one is of `next_side`.
-  auto do_row = [&](auto index, int next_side, bool there) {
+  auto do_row = [&](auto index, bool here, int next_side, bool there) {
     constexpr int side = decltype(index)::value;
     const Piece<Kind> x = next_x, g = next_g;
     if (kSides == 2 && next_side)
@@ -458,14 +495,7 @@ __global__ __launch_bounds__(NORM == LITE_ATTN_NORM_ROW ? kMaxTeam : 256) void r
         float sq = 0.f;
 #pragma unroll
         for (int e = 0; e < 4; ++e) sq += xa[e] * xa[e] + xb[e] * xb[e];  // (0 where there is no entry)
-        if constexpr (NORM == LITE_ATTN_NORM_HEAD) {
-          sq = sum_lanes(sq, p.lanes_log);
-        } else {
-          put_waves(&room, turn, f32x2{sum64(sq), 0.f});
-          lds_barrier();
-          sq = sum16(get_waves(&room, turn)[0]);
-          turn ^= 1;
-        }
+        sq = row_sum(f32x2{sq, 0.f})[0];
         const float rstd = rsqrtf(sq * inv_count + p.eps);
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
@@ -479,7 +509,7 @@ __global__ __launch_bounds__(NORM == LITE_ATTN_NORM_ROW ? kMaxTeam : 256) void r
         ra[e] = xa[e] * ca[e] - xb[e] * sa[e];
         rb[e] = xa[e] * sa[e] + xb[e] * ca[e];
       }
-      store(side, out[side], ra, rb);
+      store(side, out[side], here, ra, rb);
     } else {
       float ga[4], gb[4], za[4], zb[4];
       unpack(g, ga, gb);
@@ -496,17 +526,9 @@ __global__ __launch_bounds__(NORM == LITE_ATTN_NORM_ROW ? kMaxTeam : 256) void r
           sq += xa[e] * xa[e] + xb[e] * xb[e];
           dot += za[e] * wa[side][e] * xa[e] + zb[e] * wb[side][e] * xb[e];
         }
-        if constexpr (NORM == LITE_ATTN_NORM_HEAD) {
-          sq = sum_lanes(sq, p.lanes_log);
-          dot = sum_lanes(dot, p.lanes_log);
-        } else {
-          put_waves(&room, turn, f32x2{sum64(sq), sum64(dot)});
-          lds_barrier();
-          const f32x2 all = get_waves(&room, turn);
-          sq = sum16(all[0]);
-          dot = sum16(all[1]);
-          turn ^= 1;
-        }
+        const f32x2 all = row_sum(f32x2{sq, dot});
+        sq = all[0];
+        dot = all[1];
         // n = x rstd; dx = rstd (dn - n mean(dn n)), dn = dz w
         const float rstd = rsqrtf(sq * inv_count + p.eps);
         const float pull = rstd * rstd * (dot * inv_count);
@@ -518,22 +540,22 @@ __global__ __launch_bounds__(NORM == LITE_ATTN_NORM_ROW ? kMaxTeam : 256) void r
           zb[e] = rstd * (zb[e] * wb[side][e] - xb[e] * pull);
         }
       }
-      store(side, out[side], za, zb);
+      store(side, out[side], here, za, zb);
     }
   };
 
   const int32_t* positions = p.positions ? p.positions + batch * p.positions_stride_b : nullptr;
-  const int pairs_log = p.lanes_log + 2;          // angles of a token, with those of entries that are not turned
-  const int some = max(1, kAngles >> pairs_log);  // tokens whose angles are made at a time
+  const int each = 4 * p.lanes * p.tokens;  // angles of a tile, with those of entries that are not turned
+  const int some = kAngles / each;          // tiles whose angles are made at a time
   const bool both = kSides == 2 && p.sides == 2;
-  int made = 0, at = 0;  // tokens left of those, and where this one's start
+  int made = 0, at = 0;  // tiles left of those, and where this thread's angles of this one start
   no_stores<!WHOLE ? 8 : HALVES || kSize == 4 ? 2 : 1>(out[0].walk);
   for (int n = n0; n < p.N; n += step) {
     if (made == 0) {
       if (n != n0) lds_barrier();
       made = min(some, (p.N - 1 - n) / step + 1);
-      make_angles(p, positions, mine, n, step, made, pairs_log, angles);
-      at = 4 * c;
+      make_angles(p, positions, mine, n, step, made, angles);
+      at = 4 * (min(sub, p.tokens - 1) * p.lanes + c);
       lds_barrier();
     }
 #pragma unroll
@@ -542,11 +564,11 @@ __global__ __launch_bounds__(NORM == LITE_ATTN_NORM_ROW ? kMaxTeam : 256) void r
       ca[e] = cs[0];
       sa[e] = cs[1];
     }
-    at += 1 << pairs_log;
+    at += each;
     --made;
-    const bool more = n + step < p.N;
-    do_row(std::integral_constant<int, 0>{}, both, both || more);
-    if (both) do_row(std::integral_constant<int, kSides - 1>{}, 0, more);
+    const bool here = n + sub < p.N, more = n + step + sub < p.N;
+    do_row(std::integral_constant<int, 0>{}, here, both, both ? here : more);
+    if (both) do_row(std::integral_constant<int, kSides - 1>{}, here, 0, more);
   }
 
   if constexpr (BWD && kNormed) {
@@ -555,16 +577,15 @@ __global__ __launch_bounds__(NORM == LITE_ATTN_NORM_ROW ? kMaxTeam : 256) void r
       const RotarySide& s = sides[side];
       if (!s.part) continue;
       if constexpr (NORM == LITE_ATTN_NORM_ROW) {
-        float* to = s.part + ((size_t)share * s.heads + head) * p.head_dim;
+        float* to = s.part + (((size_t)share * p.tokens + sub) * s.heads + head) * p.head_dim;
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
           if (!valid(side, e)) continue;
           to[place_a(e)] = da[side][e];
           to[place_b(e)] = db[side][e];
         }
-      } else {  // the heads share their weights: summed in order here, a head's sums after the other's
+      } else {  // the heads share their weights: summed in order here, the tokens of the tile and their heads
         __shared__ float sums[256 * kEach];
-        const int padded = lanes * kEach;
         lds_barrier();
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
@@ -573,14 +594,15 @@ __global__ __launch_bounds__(NORM == LITE_ATTN_NORM_ROW ? kMaxTeam : 256) void r
         }
         lds_barrier();
         float* to = s.part + (size_t)block * p.head_dim;
-        if (slot == 0) {
+        if (tid < p.lanes) {
+          const int rows = p.tokens * p.team_heads;
 #pragma unroll
           for (int e = 0; e < 4; ++e) {
             if (e >= in_head) continue;
             float ta = 0.f, tb = 0.f;
-            for (int h = 0; h < p.team_heads; ++h) {
-              ta += sums[h * padded + c * kEach + 2 * e];
-              tb += sums[h * padded + c * kEach + 2 * e + 1];
+            for (int h = 0; h < rows; ++h) {
+              ta += sums[(h * p.lanes + c) * kEach + 2 * e];
+              tb += sums[(h * p.lanes + c) * kEach + 2 * e + 1];
             }
             to[place_a(e)] = ta;
             to[place_b(e)] = tb;
@@ -1113,7 +1135,7 @@ hipError_t launch_rotary_weights(const RotaryParams& p, float* dq_weight, float*
     s.part[x] = p.side[x].part;
     s.out[x] = out[x];
     s.columns[x] = out[x] ? (row ? p.side[x].heads : 1) * p.head_dim : 0;
-    s.rows[x] = p.N == 0 ? 0 : p.batch * p.shares * (row ? 1 : p.groups);
+    s.rows[x] = p.N == 0 ? 0 : p.batch * p.shares * (row ? p.tokens : p.groups);
     blocks[x] = (s.columns[x] + 63) / 64;
   }
   s.blocks0 = blocks[0];

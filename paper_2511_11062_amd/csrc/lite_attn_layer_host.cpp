@@ -88,27 +88,55 @@ int log2_up(int x) {
 }
 
 struct RotaryShape {
-  int lanes_log, team_heads, threads, shares, groups, kinds;  // kinds of workgroups
+  int lanes, team_heads, near_heads, groups, row_lanes, sum_log, tokens, threads, shares;
+  int kinds;  // of workgroups of a batch entry
 };
 
-RotaryShape rotary_shape(const lite_attn_rotary_desc_t& d, bool bwd) {
+// A head takes a thread for each kEach entries; a workgroup takes all heads of a token (NORM_ROW) or as many as 256 threads
+// hold, and, where these are few and the tokens not too far apart (`together`), several tokens: us at 302400 tokens of 2 heads
+// of 128 with a token in a wave of its own 190, of 16 tokens in a workgroup of 256 threads 96; 2 x 3913 tokens of 5 heads of 72,
+// backwards, 28 -> 20.
+RotaryShape rotary_shape(const lite_attn_rotary_desc_t& d, bool bwd, bool together) {
   RotaryShape s;
-  s.lanes_log = log2_up((d.head_dim + kEach - 1) / kEach);
-  const int most = std::max(d.heads_q, d.heads_k), lanes = 1 << s.lanes_log;
-  s.team_heads = d.norm == LITE_ATTN_NORM_ROW ? most : std::min(most, std::max(1, 256 / lanes));
-  s.threads = (s.team_heads * lanes + 63) / 64 * 64;
+  const bool by_row = d.norm == LITE_ATTN_NORM_ROW;
+  const int most = std::max(d.heads_q, d.heads_k);
+  s.lanes = (d.head_dim + kEach - 1) / kEach;
+  s.team_heads = by_row ? most : std::min(most, std::max(1, 256 / s.lanes));
   s.groups = (most + s.team_heads - 1) / s.team_heads;
+  s.row_lanes = s.team_heads * s.lanes;
+  s.sum_log = -1;
+  if (by_row && s.row_lanes <= 64) {
+    s.sum_log = log2_up(s.row_lanes);
+    s.row_lanes = 1 << s.sum_log;
+  } else if (!by_row && (s.lanes & (s.lanes - 1)) == 0) {
+    s.sum_log = log2_up(s.lanes);
+  }
+  s.tokens = together && (!by_row || s.sum_log >= 0) ? std::max(1, std::min(256 / s.row_lanes, d.seqlen)) : 1;
+  s.threads = (s.tokens * s.row_lanes + 63) / 64 * 64;
+  s.near_heads = s.tokens > 1 ? s.team_heads : std::min(s.team_heads, 64 % s.lanes ? 63 / s.lanes + 2 : 64 / s.lanes);
   s.kinds = s.groups * (rotary_sides(d.norm, bwd) == 1 && d.heads_k ? 2 : 1);
-  const int64_t row = (int64_t)s.team_heads * d.head_dim * size_of(d.dtype);
-  s.shares = shares_of((int64_t)d.batch * s.kinds, d.seqlen, s.threads / 64,
-                       bwd && d.norm != LITE_ATTN_NORM_NONE ? 2 * row : row);
+  const int64_t bytes = (int64_t)s.tokens * s.team_heads * d.head_dim * size_of(d.dtype);
+  s.shares = shares_of((int64_t)d.batch * s.kinds, (int)(((int64_t)d.seqlen + s.tokens - 1) / s.tokens), s.threads / 64,
+                       bwd && d.norm != LITE_ATTN_NORM_NONE ? 2 * bytes : bytes);
   return s;
+}
+
+// Whether what a workgroup (a wave, if it takes one token at a time) has of a tensor lies within 4 GiB: offsets have 32 bits.
+bool near(const lite_attn_heads_t& t, const lite_attn_rotary_desc_t& d, const RotaryShape& s, int heads) {
+  const int apart = std::min(heads, s.near_heads) - 1;
+  const int64_t most = (((int64_t)1 << 32) - 4096) / size_of(d.dtype) - d.head_dim;
+  if (apart > 0 && t.stride_h > most / apart) return false;
+  const int64_t left = most - (apart > 0 ? apart * t.stride_h : 0);
+  return s.tokens == 1 || t.stride_n <= left / (s.tokens - 1);
 }
 
 // Floats that one share leaves for the weights' gradient of a side.
 size_t rotary_part(const lite_attn_rotary_desc_t& d, const RotaryShape& s, int side) {
   const int heads = side ? d.heads_k : d.heads_q;
-  return (size_t)(d.norm == LITE_ATTN_NORM_ROW ? heads : heads ? s.groups : 0) * d.head_dim;
+  return (size_t)(d.norm == LITE_ATTN_NORM_ROW ? s.tokens * heads : heads ? s.groups : 0) * d.head_dim;
+}
+size_t rotary_workspace(const lite_attn_rotary_desc_t& d, const RotaryShape& s) {
+  return up16(sizeof(float) * d.batch * s.shares * (rotary_part(d, s, 0) + rotary_part(d, s, 1)));
 }
 
 int fill_rotary(const lite_attn_rotary_desc_t& d, const lite_attn_positions_t& at, const void* const weights[2],
@@ -134,12 +162,16 @@ int fill_rotary(const lite_attn_rotary_desc_t& d, const lite_attn_positions_t& a
   p->sides = d.heads_k ? 2 : 1;
   p->batch = d.batch;
   p->N = d.seqlen;
+  p->tokens = s.tokens;
   p->shares = s.shares;
   p->head_dim = d.head_dim;
   p->pairs = d.pairs;
-  p->lanes_log = s.lanes_log;
+  p->lanes = s.lanes;
   p->team_heads = s.team_heads;
   p->groups = s.groups;
+  p->near_heads = s.near_heads;
+  p->row_lanes = s.row_lanes;
+  p->sum_log = s.sum_log;
   p->norm = d.norm;
   p->halves = d.halves;
   p->weight_dtype = d.weight_dtype;
@@ -150,6 +182,10 @@ int fill_rotary(const lite_attn_rotary_desc_t& d, const lite_attn_positions_t& a
   p->eps = d.eps;
   p->per_area = reciprocal(p->area);
   p->per_width = reciprocal(p->width);
+  p->per_lanes = reciprocal(s.lanes);
+  p->per_row = reciprocal(s.row_lanes);
+  p->per_tokens = reciprocal(s.tokens);
+  p->per_angles = reciprocal(4 * s.lanes);
   return LITE_ATTN_OK;
 }
 
@@ -164,12 +200,6 @@ Lines lines(const lite_attn_rows_t& t, int dtype) {
 
 }  // namespace
 
-// A wave's heads (512 entries, of ragged heads fewer) lie within 2 GiB of each other: their offsets have 31 bits.
-static bool near(const lite_attn_heads_t& t, const lite_attn_rotary_desc_t& d, int heads) {
-  const int in_wave = std::min(heads, std::max(1, 64 >> log2_up((d.head_dim + kEach - 1) / kEach)));
-  return in_wave == 1 || t.stride_h <= (((int64_t)1 << 31) - 4096) / size_of(d.dtype) / (in_wave - 1);
-}
-
 int check_rotary(const lite_attn_rotary_desc_t* d) {
   if (!d) return LITE_ATTN_EINVAL;
   if (d->batch < 1 || d->seqlen < 0 || d->heads_q < 1 || d->heads_k < 0 || d->head_dim < 2 || d->head_dim % 2)
@@ -180,7 +210,7 @@ int check_rotary(const lite_attn_rotary_desc_t* d) {
   if ((d->halves != 0 && d->halves != 1) || d->pairs < 0 || d->pairs > d->head_dim / 2) return LITE_ATTN_EINVAL;
   if (d->grid[0] < 1 || d->grid[1] < 1 || d->grid[2] < 1 || !good_eps(d->eps)) return LITE_ATTN_EINVAL;
   if (d->head_dim > 512) return LITE_ATTN_EUNSUPPORTED;
-  const int64_t lanes = (int64_t)1 << log2_up((d->head_dim + kEach - 1) / kEach), most = std::max(d->heads_q, d->heads_k);
+  const int64_t lanes = (d->head_dim + kEach - 1) / kEach, most = std::max(d->heads_q, d->heads_k);
   if (d->norm == LITE_ATTN_NORM_ROW && most * lanes > kMaxTeam) return LITE_ATTN_EUNSUPPORTED;
   if (most > 1 << 16) return LITE_ATTN_EUNSUPPORTED;
   if ((int64_t)d->batch * d->seqlen > kMaxRows) return LITE_ATTN_EUNSUPPORTED;
@@ -190,30 +220,46 @@ int check_rotary(const lite_attn_rotary_desc_t* d) {
 }
 
 int plan_rotary(const lite_attn_rotary_desc_t& d, const lite_attn_rotary_fwd_t& a, RotaryParams* p, LayerLaunch* l) {
-  const RotaryShape s = rotary_shape(d, false);
+  const int heads[2] = {d.heads_q, d.heads_k}, sides = d.heads_k ? 2 : 1;
+  const lite_attn_heads_t in[2] = {a.q, a.k}, out[2] = {a.q_out, a.k_out};
+  RotaryShape s = rotary_shape(d, false, true);
+  for (int x = 0; x < sides; ++x) {
+    if (!good(view(in[x], d, heads[x]), false) || !good(view(out[x], d, heads[x]), true)) return LITE_ATTN_EINVAL;
+    if (!near(in[x], d, s, heads[x]) || !near(out[x], d, s, heads[x])) s = rotary_shape(d, false, false);
+  }
+  for (int x = 0; x < sides; ++x)
+    if (!near(in[x], d, s, heads[x]) || !near(out[x], d, s, heads[x])) return LITE_ATTN_EUNSUPPORTED;
   const void* const weights[2] = {a.q_weight, a.k_weight};
   const int rc = fill_rotary(d, a.at, weights, s, p);
   if (rc != LITE_ATTN_OK) return rc;
-  for (int x = 0; x < (d.heads_k ? 2 : 1); ++x) {
-    const lite_attn_heads_t &in = x ? a.k : a.q, &out = x ? a.k_out : a.q_out;
-    const View vi = view(in, d, p->side[x].heads), vo = view(out, d, p->side[x].heads);
-    if (!good(vi, false) || !good(vo, true)) return LITE_ATTN_EINVAL;
-    if (!near(in, d, p->side[x].heads) || !near(out, d, p->side[x].heads)) return LITE_ATTN_EUNSUPPORTED;
-    p->side[x].x = static_cast<const char*>(in.data);
-    p->side[x].out = static_cast<char*>(out.data);
-    set(p->side[x].xs, in, d.dtype);
-    set(p->side[x].os, out, d.dtype);
+  for (int x = 0; x < sides; ++x) {
+    p->side[x].x = static_cast<const char*>(in[x].data);
+    p->side[x].out = static_cast<char*>(out[x].data);
+    set(p->side[x].xs, in[x], d.dtype);
+    set(p->side[x].os, out[x], d.dtype);
   }
   return launch_of(d.batch, (int64_t)s.shares * s.kinds, s.threads, l);
 }
 
 int plan_rotary(const lite_attn_rotary_desc_t& d, const lite_attn_rotary_bwd_t& a, RotaryParams* p, LayerLaunch* l) {
-  const RotaryShape s = rotary_shape(d, true);
-  const void* const weights[2] = {a.q_weight, a.k_weight};
+  const int heads[2] = {d.heads_q, d.heads_k}, sides = d.heads_k ? 2 : 1;
+  const lite_attn_heads_t in[2] = {a.q, a.k}, g[2] = {a.dq_out, a.dk_out}, out[2] = {a.dq, a.dk};
   float* const grads[2] = {a.dq_weight, a.dk_weight};
+  const bool normed = d.norm != LITE_ATTN_NORM_NONE;
+  RotaryShape s = rotary_shape(d, true, true);
+  auto all_near = [&](int x) {
+    return (!normed || near(in[x], d, s, heads[x])) && near(g[x], d, s, heads[x]) && near(out[x], d, s, heads[x]);
+  };
+  for (int x = 0; x < sides; ++x) {
+    if (normed && !good(view(in[x], d, heads[x]), false)) return LITE_ATTN_EINVAL;
+    if (!good(view(g[x], d, heads[x]), false) || !good(view(out[x], d, heads[x]), true)) return LITE_ATTN_EINVAL;
+    if (!all_near(x)) s = rotary_shape(d, true, false);
+  }
+  for (int x = 0; x < sides; ++x)
+    if (!all_near(x)) return LITE_ATTN_EUNSUPPORTED;
+  const void* const weights[2] = {a.q_weight, a.k_weight};
   const int rc = fill_rotary(d, a.at, weights, s, p);
   if (rc != LITE_ATTN_OK) return rc;
-  const bool normed = d.norm != LITE_ATTN_NORM_NONE;
   if (!normed && (grads[0] || grads[1])) return LITE_ATTN_EINVAL;
   if (!good_grad(grads[0]) || !good_grad(grads[1])) return LITE_ATTN_EINVAL;
   if (grads[0] || grads[1]) {
@@ -221,18 +267,13 @@ int plan_rotary(const lite_attn_rotary_desc_t& d, const lite_attn_rotary_bwd_t& 
       return LITE_ATTN_EWORKSPACE;
   }
   float* part = static_cast<float*>(a.workspace);
-  for (int x = 0; x < (d.heads_k ? 2 : 1); ++x) {
-    const lite_attn_heads_t &in = x ? a.k : a.q, &g = x ? a.dk_out : a.dq_out, &out = x ? a.dk : a.dq;
-    const View vi = view(in, d, p->side[x].heads), vg = view(g, d, p->side[x].heads), vo = view(out, d, p->side[x].heads);
-    if ((normed && !good(vi, false)) || !good(vg, false) || !good(vo, true)) return LITE_ATTN_EINVAL;
-    if ((normed && !near(in, d, p->side[x].heads)) || !near(g, d, p->side[x].heads) || !near(out, d, p->side[x].heads))
-      return LITE_ATTN_EUNSUPPORTED;
-    p->side[x].x = static_cast<const char*>(in.data);
-    p->side[x].g = static_cast<const char*>(g.data);
-    p->side[x].out = static_cast<char*>(out.data);
-    set(p->side[x].xs, in, d.dtype);
-    set(p->side[x].gs, g, d.dtype);
-    set(p->side[x].os, out, d.dtype);
+  for (int x = 0; x < sides; ++x) {
+    p->side[x].x = static_cast<const char*>(in[x].data);
+    p->side[x].g = static_cast<const char*>(g[x].data);
+    p->side[x].out = static_cast<char*>(out[x].data);
+    set(p->side[x].xs, in[x], d.dtype);
+    set(p->side[x].gs, g[x], d.dtype);
+    set(p->side[x].os, out[x], d.dtype);
     if (grads[x]) p->side[x].part = part;
     part += (size_t)d.batch * s.shares * rotary_part(d, s, x);
   }
@@ -366,8 +407,9 @@ extern "C" {
 
 size_t lite_attn_rotary_bwd_workspace(const lite_attn_rotary_desc_t* desc) {
   if (la::check_rotary(desc) != LITE_ATTN_OK || desc->norm == LITE_ATTN_NORM_NONE) return 0;
-  const la::RotaryShape s = la::rotary_shape(*desc, true);
-  return la::up16(sizeof(float) * desc->batch * s.shares * (la::rotary_part(*desc, s, 0) + la::rotary_part(*desc, s, 1)));
+  // (which of the two shapes a call takes depends on its strides)
+  return std::max(la::rotary_workspace(*desc, la::rotary_shape(*desc, true, true)),
+                  la::rotary_workspace(*desc, la::rotary_shape(*desc, true, false)));
 }
 
 size_t lite_attn_residual_norm_bwd_workspace(const lite_attn_residual_desc_t* desc) {

@@ -24,7 +24,8 @@ struct RotarySide {
   char* out;          // result (backwards: gradient of the input)
   int64_t xs[3], gs[3], os[3];  // strides over batch, heads, tokens, bytes
   const void* w;      // weights or null
-  float* part;        // backwards: [batch * shares][heads or groups][head_dim] sums for the weights' gradient, or null
+  float* part;        // backwards: sums for the weights' gradient, [batch * shares][tokens][heads][head_dim] or, of weights
+                      //   that the heads share, [batch * shares][groups][head_dim]; or null
   float inv_count;    // 1 / entries that a norm goes over
   int heads;
 };
@@ -39,15 +40,19 @@ struct RotaryParams {
   const int32_t* positions;
   int64_t positions_stride_b;
   int batch, N;
-  int shares;            // share x of a batch entry: tokens x, x + shares, x + 2 shares, ...
+  int tokens;            // neighbouring tokens that a workgroup takes at a time, a tile
+  int shares;            // share x of a batch entry: tiles x, x + shares, x + 2 shares, ...
   int head_dim, pairs;
-  int lanes_log;         // a head takes 1 << lanes_log threads of kEach entries
+  int lanes;             // threads of a head
   int team_heads;        // heads that a workgroup takes, of q and of k
   int groups;            // of as many heads
+  int near_heads;        // heads that offsets from one place reach: the workgroup's or, if it takes one token, a wave's
+  int row_lanes;         // threads of a token: of its heads, under NORM_ROW up to 64 rounded up to a power of two
+  int sum_log;           // sums go over 1 << sum_log neighbouring lanes; -1: over all waves (NORM_ROW), or by way of LDS
   int norm, halves, weight_dtype;
   int token_start, area, width, video;  // area = height * width, video = frames * area
   float eps;
-  uint32_t per_area, per_width;         // reciprocals for quotient()
+  uint32_t per_area, per_width, per_lanes, per_row, per_tokens, per_angles;  // reciprocals for quotient()
 };
 
 // Rows of a tensor: the first of the first batch entry, and strides over batch entries and rows, bytes.
