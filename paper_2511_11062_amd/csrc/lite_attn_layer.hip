@@ -139,27 +139,30 @@ struct Piece {
       }
     }
   }
+  template <int kPolicy = kStreamed>
   __device__ __forceinline__ void store_run(int run, Buffer to, int offset) const {
     if constexpr (kNarrow)
-      __builtin_amdgcn_raw_buffer_store_b64(u32x2{w[2 * run], w[2 * run + 1]}, to, offset, 0, kStreamed);
+      __builtin_amdgcn_raw_buffer_store_b64(u32x2{w[2 * run], w[2 * run + 1]}, to, offset, 0, kPolicy);
     else
-      __builtin_amdgcn_raw_buffer_store_b128(u32x4{w[4 * run], w[4 * run + 1], w[4 * run + 2], w[4 * run + 3]}, to, offset, 0, kStreamed);
+      __builtin_amdgcn_raw_buffer_store_b128(u32x4{w[4 * run], w[4 * run + 1], w[4 * run + 2], w[4 * run + 3]}, to, offset, 0, kPolicy);
   }
+  template <int kPolicy = kStreamed>
   __device__ __forceinline__ void store(Buffer to, int offset) const {
     if constexpr (kNarrow) {
-      __builtin_amdgcn_raw_buffer_store_b128(u32x4{w[0], w[1], w[2], w[3]}, to, offset, 0, kStreamed);
+      __builtin_amdgcn_raw_buffer_store_b128(u32x4{w[0], w[1], w[2], w[3]}, to, offset, 0, kPolicy);
     } else {
-      store_run(0, to, offset);
-      store_run(1, to, offset + 16);
+      store_run<kPolicy>(0, to, offset);
+      store_run<kPolicy>(1, to, offset + 16);
     }
   }
+  template <int kPolicy = kStreamed>
   __device__ __forceinline__ void store_two(int e, Buffer to, int offset0, int offset1) const {
     if constexpr (kNarrow) {
-      __builtin_amdgcn_raw_buffer_store_b16((uint16_t)w[e / 2], to, offset0, 0, kStreamed);
-      __builtin_amdgcn_raw_buffer_store_b16((uint16_t)(w[e / 2] >> 16), to, offset1, 0, kStreamed);
+      __builtin_amdgcn_raw_buffer_store_b16((uint16_t)w[e / 2], to, offset0, 0, kPolicy);
+      __builtin_amdgcn_raw_buffer_store_b16((uint16_t)(w[e / 2] >> 16), to, offset1, 0, kPolicy);
     } else {
-      __builtin_amdgcn_raw_buffer_store_b32(w[e], to, offset0, 0, kStreamed);
-      __builtin_amdgcn_raw_buffer_store_b32(w[e + 1], to, offset1, 0, kStreamed);
+      __builtin_amdgcn_raw_buffer_store_b32(w[e], to, offset0, 0, kPolicy);
+      __builtin_amdgcn_raw_buffer_store_b32(w[e + 1], to, offset1, 0, kPolicy);
     }
   }
 };
@@ -236,6 +239,13 @@ __device__ __forceinline__ void touch_arguments() {
   asm volatile("" ::"s"(x));
 }
 
+// x, of which the compiler does not know that it is the same for each row: what follows from it is made where it is needed, and
+// not kept in a register each for all rows.
+__device__ __forceinline__ int afresh(int x) {
+  asm volatile("" : "+v"(x));
+  return x;
+}
+
 // Where a token stands.
 struct Position {
   int at[3];
@@ -308,8 +318,12 @@ __global__ __launch_bounds__(NORM == LITE_ATTN_NORM_ROW ? kMaxTeam : 256) void r
   __shared__ WaveRoom room;
   __shared__ f32x2 lane_sums[2][NORM == LITE_ATTN_NORM_HEAD ? 256 + 64 : 1];  // (threads of no head read on behind 256)
   const int tid = threadIdx.x;
-  const int block = kSides == 2 ? (int)blockIdx.x : (int)blockIdx.x / p.sides;
-  const RotarySide* const sides = p.side + (kSides == 2 ? 0 : (int)blockIdx.x - block * p.sides);
+  // Workgroups go to the XCDs in turn.  Where neighbouring tokens share lines, an XCD takes neighbouring shares, and its cache
+  // keeps a result's line until the others have written their parts of it.
+  const int per_xcd = (int)gridDim.x >> 3, rest = (int)gridDim.x & 7, xcd = (int)blockIdx.x & 7;
+  const int place = p.shared_reads ? xcd * per_xcd + min(xcd, rest) + ((int)blockIdx.x >> 3) : (int)blockIdx.x;
+  const int block = kSides == 2 ? place : place / p.sides;
+  const RotarySide* const sides = p.side + (kSides == 2 ? 0 : place - block * p.sides);
   const int share = block / p.groups, group = block - share * p.groups;
   const int batch = share / p.shares, n0 = (share - batch * p.shares) * p.tokens, step = p.shares * p.tokens;
 
@@ -358,8 +372,9 @@ __global__ __launch_bounds__(NORM == LITE_ATTN_NORM_ROW ? kMaxTeam : 256) void r
     } else {
 #pragma unroll
       for (int e = 0; e < 4; ++e) {
-        const int a = there && valid(side, e) ? t.first + (place_a(e) - first) * kSize : t.walk.bytes;
-        const int b = there && valid(side, e) ? t.first + (place_b(e) - first) * kSize : t.walk.bytes;
+        const int at = afresh(t.first);
+        const int a = there && valid(side, e) ? at + (place_a(e) - first) * kSize : t.walk.bytes;
+        const int b = there && valid(side, e) ? at + (place_b(e) - first) * kSize : t.walk.bytes;
         to.load_two(2 * e, from, a, b);
       }
     }
@@ -384,19 +399,27 @@ __global__ __launch_bounds__(NORM == LITE_ATTN_NORM_ROW ? kMaxTeam : 256) void r
     }
     Piece<Kind> out;
     out.pack(x);
-    if constexpr (WHOLE && HALVES) {
-      out.store_run(0, to, there ? t.first : t.walk.bytes);
-      out.store_run(1, to, there ? t.second : t.walk.bytes);
-    } else if constexpr (WHOLE) {
-      out.store(to, there ? t.first : t.walk.bytes);
-    } else {
+    auto put = [&](auto policy) {
+      constexpr int kPolicy = decltype(policy)::value;
+      if constexpr (WHOLE && HALVES) {
+        out.template store_run<kPolicy>(0, to, there ? t.first : t.walk.bytes);
+        out.template store_run<kPolicy>(1, to, there ? t.second : t.walk.bytes);
+      } else if constexpr (WHOLE) {
+        out.template store<kPolicy>(to, there ? t.first : t.walk.bytes);
+      } else {
 #pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        const int a = there && valid(side, e) ? t.first + (place_a(e) - first) * kSize : t.walk.bytes;
-        const int b = there && valid(side, e) ? t.first + (place_b(e) - first) * kSize : t.walk.bytes;
-        out.store_two(2 * e, to, a, b);
+        for (int e = 0; e < 4; ++e) {
+          const int at = afresh(t.first);
+          const int a = there && valid(side, e) ? at + (place_a(e) - first) * kSize : t.walk.bytes;
+          const int b = there && valid(side, e) ? at + (place_b(e) - first) * kSize : t.walk.bytes;
+          out.template store_two<kPolicy>(2 * e, to, a, b);
+        }
       }
-    }
+    };
+    if (p.shared_writes)
+      put(std::integral_constant<int, 0>{});
+    else
+      put(std::integral_constant<int, kStreamed>{});
   };
 
   Tensor in_x[kSides], in_g[kSides], out[kSides];

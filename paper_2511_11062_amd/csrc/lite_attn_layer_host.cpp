@@ -189,6 +189,9 @@ int fill_rotary(const lite_attn_rotary_desc_t& d, const lite_attn_positions_t& a
   return LITE_ATTN_OK;
 }
 
+// Whether the entries of neighbouring tokens share a line of memory.
+bool shares_lines(const lite_attn_heads_t& t, const lite_attn_rotary_desc_t& d) { return t.stride_n * size_of(d.dtype) % 128 != 0; }
+
 void set(int64_t to[3], const lite_attn_heads_t& t, int dtype) {
   to[0] = t.stride_b * size_of(dtype);
   to[1] = t.stride_h * size_of(dtype);
@@ -237,6 +240,8 @@ int plan_rotary(const lite_attn_rotary_desc_t& d, const lite_attn_rotary_fwd_t& 
     p->side[x].out = static_cast<char*>(out[x].data);
     set(p->side[x].xs, in[x], d.dtype);
     set(p->side[x].os, out[x], d.dtype);
+    p->shared_writes |= shares_lines(out[x], d);
+    p->shared_reads |= p->shared_writes | shares_lines(in[x], d);
   }
   return launch_of(d.batch, (int64_t)s.shares * s.kinds, s.threads, l);
 }
@@ -274,6 +279,8 @@ int plan_rotary(const lite_attn_rotary_desc_t& d, const lite_attn_rotary_bwd_t& 
     set(p->side[x].xs, in[x], d.dtype);
     set(p->side[x].gs, g[x], d.dtype);
     set(p->side[x].os, out[x], d.dtype);
+    p->shared_writes |= shares_lines(out[x], d);
+    p->shared_reads |= p->shared_writes | shares_lines(g[x], d) | (normed && shares_lines(in[x], d));
     if (grads[x]) p->side[x].part = part;
     part += (size_t)d.batch * s.shares * rotary_part(d, s, x);
   }

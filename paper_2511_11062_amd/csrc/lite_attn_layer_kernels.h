@@ -50,6 +50,7 @@ struct RotaryParams {
   int row_lanes;         // threads of a token: of its heads, under NORM_ROW up to 64 rounded up to a power of two
   int sum_log;           // sums go over 1 << sum_log neighbouring lanes; -1: over all waves (NORM_ROW), or by way of LDS
   int norm, halves, weight_dtype;
+  int shared_reads, shared_writes;  // neighbouring tokens share lines of memory, of an input or a result; of a result
   int token_start, area, width, video;  // area = height * width, video = frames * area
   float eps;
   uint32_t per_area, per_width, per_lanes, per_row, per_tokens, per_angles;  // reciprocals for quotient()
