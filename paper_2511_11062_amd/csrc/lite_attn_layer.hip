@@ -192,15 +192,28 @@ __device__ __forceinline__ float sum16(float x) {
   return add_dpp<kMirror>(add_dpp<kHalfMirror>(add_dpp<kXor2>(add_dpp<kXor1>(x))));
 }
 __device__ __forceinline__ float sum64(float x) { return add_halves(add_row_pairs(sum16(x))); }
-// Sum over 1 << log neighbouring lanes, in all of them.
+// Sum over 1 << log neighbouring lanes, in all of them: six steps, those that are too many adding 0.
+template <int kStep>
+__device__ __forceinline__ float step_of(float x) {
+  if constexpr (kStep == 4) {
+    const u32x2 s = __builtin_amdgcn_permlane16_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+    return __uint_as_float(threadIdx.x & 16 ? s[0] : s[1]);
+  } else if constexpr (kStep == 5) {
+    const u32x2 s = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+    return __uint_as_float(threadIdx.x & 32 ? s[0] : s[1]);
+  } else {
+    constexpr int kCtrl = kStep == 0 ? kXor1 : kStep == 1 ? kXor2 : kStep == 2 ? kHalfMirror : kMirror;
+    return __uint_as_float(__builtin_amdgcn_update_dpp(0u, __float_as_uint(x), kCtrl, 0xf, 0xf, true));
+  }
+}
+template <int kStep = 0>
 __device__ __forceinline__ float sum_lanes(float x, int log) {
-  if (log >= 1) x = add_dpp<kXor1>(x);
-  if (log >= 2) x = add_dpp<kXor2>(x);
-  if (log >= 3) x = add_dpp<kHalfMirror>(x);
-  if (log >= 4) x = add_dpp<kMirror>(x);
-  if (log >= 5) x = add_row_pairs(x);
-  if (log >= 6) x = add_halves(x);
-  return x;
+  if constexpr (kStep < 6) {
+    const uint32_t on = log > kStep ? 0xffffffffu : 0u;
+    return sum_lanes<kStep + 1>(x + __uint_as_float(__float_as_uint(step_of<kStep>(x)) & on), log);
+  } else {
+    return x;
+  }
 }
 
 // A barrier that orders LDS alone: loads and stores of global memory stay in flight across it.
@@ -246,16 +259,28 @@ __device__ __forceinline__ int afresh(int x) {
   return x;
 }
 
+// A kernel's arguments where they lie, to be read there again: what is needed once for many rows takes no scalar registers in
+// between.
+typedef const __attribute__((address_space(4))) RotaryParams* RotaryArgs;
+__device__ __forceinline__ RotaryArgs rotary_args() {
+  RotaryArgs a = (RotaryArgs)__builtin_amdgcn_kernarg_segment_ptr();
+  asm volatile("" : "+s"(a));
+  return a;
+}
+
 // Where a token stands.
 struct Position {
   int at[3];
 };
-__device__ __forceinline__ Position position_of(const RotaryParams& p, const int32_t* positions, int n) {
-  if (positions) return {{positions[n], positions[n + (int64_t)p.N], positions[n + 2 * (int64_t)p.N]}};
-  int t = p.token_start + n;
-  if (t >= p.video) t = 0;
-  const int f = quotient(t, p.area, p.per_area), in = t - f * p.area, y = quotient(in, p.width, p.per_width);
-  return {{f, y, in - y * p.width}};
+__device__ __forceinline__ Position position_of(RotaryArgs p, int batch, int n) {
+  if (p->positions) {
+    const int32_t* const at = p->positions + batch * p->positions_stride_b + n;
+    return {{at[0], at[(int64_t)p->N], at[2 * (int64_t)p->N]}};
+  }
+  int t = p->token_start + n;
+  if (t >= p->video) t = 0;
+  const int f = quotient(t, p->area, p->per_area), in = t - f * p->area, y = quotient(in, p->width, p->per_width);
+  return {{f, y, in - y * p->width}};
 }
 
 // How fast a pair turns, and its cos and sin at a position.  In 64 bits until whole turns are off: in 32 an angle of 10^5
@@ -263,9 +288,10 @@ __device__ __forceinline__ Position position_of(const RotaryParams& p, const int
 struct Speed {
   double f[3];
 };
-__device__ __forceinline__ Speed speed_of(const RotaryParams& p, int pair) {
-  if (pair >= p.pairs) return {{0.0, 0.0, 0.0}};
-  return {{p.freqs[pair], p.freqs[p.pairs + pair], p.freqs[2 * p.pairs + pair]}};
+__device__ __forceinline__ Speed speed_of(RotaryArgs p, int pair) {
+  const int pairs = p->pairs;
+  if (pair >= pairs) return {{0.0, 0.0, 0.0}};
+  return {{p->freqs[pair], p->freqs[pairs + pair], p->freqs[2 * pairs + pair]}};
 }
 __device__ __forceinline__ f32x2 angle_of(const Speed& v, const Position& at) {
   double turns = (double)at.at[0] * v.f[0];
@@ -281,24 +307,24 @@ __device__ __forceinline__ f32x2 angle_of(const Speed& v, const Position& at) {
 // The angles of `tiles` tiles of tokens, the first of them at token n, `step` tokens from one to the next: 4 * lanes for each
 // token.  If those are whole waves, a wave takes a token, whose position it finds by scalar instructions, and a thread keeps its
 // pair (`mine`: how fast pair threadIdx.x % 64 turns).
-__device__ __forceinline__ void make_angles(const RotaryParams& p, const int32_t* positions, const Speed& mine, int n, int step,
-                                            int tiles, f32x2* angles) {
-  const int each = 4 * p.lanes, tokens = tiles * p.tokens;
+__device__ __forceinline__ void make_angles(const Speed& mine, int batch, int n, int step, int tiles, f32x2* angles) {
+  const RotaryArgs p = rotary_args();
+  const int each = 4 * p->lanes, tokens = tiles * p->tokens;
   auto token = [&](int x) {  // (of the last tile some may be none)
-    const int tile = quotient(x, p.tokens, p.per_tokens);
-    return min(p.N - 1, n + tile * step + (x - tile * p.tokens));
+    const int tile = quotient(x, p->tokens, p->per_tokens);
+    return min(p->N - 1, n + tile * step + (x - tile * p->tokens));
   };
   if (each % 64 == 0) {
     const int waves = blockDim.x >> 6, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
     for (int first = 0; first < each; first += 64) {
       const Speed v = first == 0 ? mine : speed_of(p, first + lane);
       for (int x = wave; x < tokens; x += waves)
-        angles[x * each + first + lane] = angle_of(v, position_of(p, positions, token(x)));
+        angles[x * each + first + lane] = angle_of(v, position_of(p, batch, token(x)));
     }
   } else {
     for (int x = threadIdx.x; x < tokens * each; x += blockDim.x) {
-      const int t = quotient(x, each, p.per_angles);
-      angles[x] = angle_of(speed_of(p, x - t * each), position_of(p, positions, token(t)));
+      const int t = quotient(x, each, p->per_angles);
+      angles[x] = angle_of(speed_of(p, x - t * each), position_of(p, batch, token(t)));
     }
   }
 }
@@ -308,22 +334,23 @@ __device__ __forceinline__ void make_angles(const RotaryParams& p, const int32_t
 // for their gradient would need 32 registers, a workgroup takes q or k.)  A thread holds four pairs of a head, a[4] and b[4].
 // WHOLE: they are eight entries in a row or, of turned halves, four and four; otherwise (a head's ragged end, four pairs across
 // the end of the turned halves) every entry is fetched by itself.
-template <class Kind, bool HALVES, bool WHOLE, int NORM, bool BWD>
-__global__ __launch_bounds__(NORM == LITE_ATTN_NORM_ROW ? kMaxTeam : 256) void rotary_kernel(const RotaryParams p) {
+template <class Kind, bool HALVES, bool WHOLE, Sums SUMS, bool BWD>
+__global__ __launch_bounds__(SUMS == kSumWaves ? kMaxTeam : 256) void rotary_kernel(const RotaryParams p) {
   constexpr int kSize = Piece<Kind>::kSize;
-  constexpr bool kNormed = NORM != LITE_ATTN_NORM_NONE;
-  constexpr int kSides = rotary_sides(NORM, BWD);
+  constexpr bool kNormed = SUMS != kSumNone;
+  constexpr int kSides = rotary_sides(kNormed, BWD);
   touch_arguments<sizeof(RotaryParams)>();
   __shared__ f32x2 angles[kAngles];
   __shared__ WaveRoom room;
-  __shared__ f32x2 lane_sums[2][NORM == LITE_ATTN_NORM_HEAD ? 256 + 64 : 1];  // (threads of no head read on behind 256)
+  __shared__ f32x2 lane_sums[2][SUMS == kSumHeads ? 256 + 64 : 1];  // (threads of no head read on behind 256)
   const int tid = threadIdx.x;
   // Workgroups go to the XCDs in turn.  Where neighbouring tokens share lines, an XCD takes neighbouring shares, and its cache
   // keeps a result's line until the others have written their parts of it.
   const int per_xcd = (int)gridDim.x >> 3, rest = (int)gridDim.x & 7, xcd = (int)blockIdx.x & 7;
   const int place = p.shared_reads ? xcd * per_xcd + min(xcd, rest) + ((int)blockIdx.x >> 3) : (int)blockIdx.x;
   const int block = kSides == 2 ? place : place / p.sides;
-  const RotarySide* const sides = p.side + (kSides == 2 ? 0 : place - block * p.sides);
+  const int which = kSides == 2 ? 0 : place - block * p.sides;  // of q and k
+  const RotarySide* const sides = p.side + which;
   const int share = block / p.groups, group = block - share * p.groups;
   const int batch = share / p.shares, n0 = (share - batch * p.shares) * p.tokens, step = p.shares * p.tokens;
 
@@ -436,7 +463,7 @@ __global__ __launch_bounds__(NORM == LITE_ATTN_NORM_ROW ? kMaxTeam : 256) void r
     if constexpr (BWD) fetch(side, in_g[side], there, next_g);
   };
   fetch_next(0, n0 + sub < p.N);
-  const Speed mine = speed_of(p, tid & 63);      // (asked for before anything is waited for)
+  const Speed mine = speed_of(rotary_args(), tid & 63);      // (asked for before anything is waited for)
   float wa[kSides][4], wb[kSides][4], da[kSides][4], db[kSides][4];  // weights and, backwards, the sums for their gradient
   if constexpr (kNormed) {
     auto load_weights = [&](auto kind) {
@@ -444,10 +471,10 @@ __global__ __launch_bounds__(NORM == LITE_ATTN_NORM_ROW ? kMaxTeam : 256) void r
       Weights v[kSides];
 #pragma unroll
       for (int side = 0; side < kSides; ++side) {
-        const int heads = NORM == LITE_ATTN_NORM_ROW ? sides[side].heads : 1;
+        const int heads = p.by_row ? sides[side].heads : 1;
         const int bytes = sides[side].w ? heads * p.head_dim * Weights::kSize : 0;
         const Buffer from = Walk{(char*)sides[side].w, 0, bytes}.row();
-        const int row = NORM == LITE_ATTN_NORM_ROW ? head * p.head_dim : 0;
+        const int row = p.by_row ? head * p.head_dim : 0;
 #pragma unroll
         for (int e = 0; e < kEach && !WHOLE; e += 2)
           v[side].load_two(e, from, valid(side, e / 2) ? (row + place_a(e / 2)) * Weights::kSize : bytes,
@@ -476,15 +503,13 @@ __global__ __launch_bounds__(NORM == LITE_ATTN_NORM_ROW ? kMaxTeam : 256) void r
   }
   int turn = 0;
   float ca[4], sa[4];
-  // Sums over what a norm goes over: neighbouring lanes, a power of two of them; all waves; or the lanes of a head, of which each
-  // adds up all from LDS.
+  // Sums over what the norm goes over (kSumHeads: each lane of a head adds up all of them from LDS).
   auto row_sum = [&](f32x2 x) {
-    if (p.sum_log >= 0) {
+    if constexpr (SUMS == kSumLanes) {
       x[0] = sum_lanes(x[0], p.sum_log);
       if constexpr (BWD) x[1] = sum_lanes(x[1], p.sum_log);
       return x;
-    }
-    if constexpr (NORM == LITE_ATTN_NORM_ROW) {
+    } else if constexpr (SUMS == kSumWaves) {
       x[0] = sum64(x[0]);
       if constexpr (BWD) x[1] = sum64(x[1]);
       put_waves(&room, turn, x);
@@ -567,7 +592,6 @@ __global__ __launch_bounds__(NORM == LITE_ATTN_NORM_ROW ? kMaxTeam : 256) void r
     }
   };
 
-  const int32_t* positions = p.positions ? p.positions + batch * p.positions_stride_b : nullptr;
   const int each = 4 * p.lanes * p.tokens;  // angles of a tile, with those of entries that are not turned
   const int some = kAngles / each;          // tiles whose angles are made at a time
   const bool both = kSides == 2 && p.sides == 2;
@@ -577,7 +601,7 @@ __global__ __launch_bounds__(NORM == LITE_ATTN_NORM_ROW ? kMaxTeam : 256) void r
     if (made == 0) {
       if (n != n0) lds_barrier();
       made = min(some, (p.N - 1 - n) / step + 1);
-      make_angles(p, positions, mine, n, step, made, angles);
+      make_angles(mine, batch, n, step, made, angles);
       at = 4 * (min(sub, p.tokens - 1) * p.lanes + c);
       lds_barrier();
     }
@@ -597,17 +621,18 @@ __global__ __launch_bounds__(NORM == LITE_ATTN_NORM_ROW ? kMaxTeam : 256) void r
   if constexpr (BWD && kNormed) {
 #pragma unroll
     for (int side = 0; side < kSides; ++side) {
-      const RotarySide& s = sides[side];
-      if (!s.part) continue;
-      if constexpr (NORM == LITE_ATTN_NORM_ROW) {
-        float* to = s.part + (((size_t)share * p.tokens + sub) * s.heads + head) * p.head_dim;
+      const RotaryArgs args = rotary_args();
+      const auto* const s = args->side + (which + side);
+      if (!s->part) continue;
+      if (args->by_row) {
+        float* to = s->part + (((size_t)share * args->tokens + sub) * s->heads + head) * args->head_dim;
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
           if (!valid(side, e)) continue;
           to[place_a(e)] = da[side][e];
           to[place_b(e)] = db[side][e];
         }
-      } else {  // the heads share their weights: summed in order here, the tokens of the tile and their heads
+      } else if constexpr (SUMS != kSumWaves) {  // the heads share their weights: summed in order here, the tokens of the tile and their heads
         __shared__ float sums[256 * kEach];
         lds_barrier();
 #pragma unroll
@@ -616,16 +641,16 @@ __global__ __launch_bounds__(NORM == LITE_ATTN_NORM_ROW ? kMaxTeam : 256) void r
           sums[tid * kEach + 2 * e + 1] = valid(side, e) ? db[side][e] : 0.f;
         }
         lds_barrier();
-        float* to = s.part + (size_t)block * p.head_dim;
-        if (tid < p.lanes) {
-          const int rows = p.tokens * p.team_heads;
+        float* to = s->part + (size_t)block * args->head_dim;
+        if (tid < args->lanes) {
+          const int rows = args->tokens * args->team_heads;
 #pragma unroll
           for (int e = 0; e < 4; ++e) {
             if (e >= in_head) continue;
             float ta = 0.f, tb = 0.f;
             for (int h = 0; h < rows; ++h) {
-              ta += sums[(h * p.lanes + c) * kEach + 2 * e];
-              tb += sums[(h * p.lanes + c) * kEach + 2 * e + 1];
+              ta += sums[(h * args->lanes + c) * kEach + 2 * e];
+              tb += sums[(h * args->lanes + c) * kEach + 2 * e + 1];
             }
             to[place_a(e)] = ta;
             to[place_b(e)] = tb;
@@ -1102,21 +1127,23 @@ __global__ __launch_bounds__(1024) void weight_sums_kernel(const ResidualParams 
 }
 
 template <class Kind, bool HALVES, bool WHOLE, bool BWD>
-void launch_rotary_norm(const RotaryParams& p, const LayerLaunch& l, hipStream_t st) {
-  if (p.norm == LITE_ATTN_NORM_NONE)
-    rotary_kernel<Kind, HALVES, WHOLE, LITE_ATTN_NORM_NONE, BWD><<<l.blocks, l.threads, 0, st>>>(p);
-  else if (p.norm == LITE_ATTN_NORM_HEAD)
-    rotary_kernel<Kind, HALVES, WHOLE, LITE_ATTN_NORM_HEAD, BWD><<<l.blocks, l.threads, 0, st>>>(p);
+void launch_rotary_sums(const RotaryParams& p, const LayerLaunch& l, hipStream_t st) {
+  if (l.sums == kSumNone)
+    rotary_kernel<Kind, HALVES, WHOLE, kSumNone, BWD><<<l.blocks, l.threads, 0, st>>>(p);
+  else if (l.sums == kSumLanes)
+    rotary_kernel<Kind, HALVES, WHOLE, kSumLanes, BWD><<<l.blocks, l.threads, 0, st>>>(p);
+  else if (l.sums == kSumHeads)
+    rotary_kernel<Kind, HALVES, WHOLE, kSumHeads, BWD><<<l.blocks, l.threads, 0, st>>>(p);
   else
-    rotary_kernel<Kind, HALVES, WHOLE, LITE_ATTN_NORM_ROW, BWD><<<l.blocks, l.threads, 0, st>>>(p);
+    rotary_kernel<Kind, HALVES, WHOLE, kSumWaves, BWD><<<l.blocks, l.threads, 0, st>>>(p);
 }
 template <class Kind, bool BWD>
 void launch_rotary_way(const RotaryParams& p, const LayerLaunch& l, hipStream_t st) {
   const bool whole = p.head_dim % kEach == 0 && (!p.halves || p.pairs % 4 == 0);
   if (p.halves)
-    whole ? launch_rotary_norm<Kind, true, true, BWD>(p, l, st) : launch_rotary_norm<Kind, true, false, BWD>(p, l, st);
+    whole ? launch_rotary_sums<Kind, true, true, BWD>(p, l, st) : launch_rotary_sums<Kind, true, false, BWD>(p, l, st);
   else
-    whole ? launch_rotary_norm<Kind, false, true, BWD>(p, l, st) : launch_rotary_norm<Kind, false, false, BWD>(p, l, st);
+    whole ? launch_rotary_sums<Kind, false, true, BWD>(p, l, st) : launch_rotary_sums<Kind, false, false, BWD>(p, l, st);
 }
 template <class Kind>
 void launch_rotary_kind(const RotaryParams& p, const LayerLaunch& l, bool bwd, hipStream_t st) {
@@ -1154,7 +1181,7 @@ hipError_t launch_rotary_weights(const RotaryParams& p, float* dq_weight, float*
   float* const out[2] = {dq_weight, dk_weight};
   int blocks[2];
   for (int x = 0; x < 2; ++x) {
-    const bool row = p.norm == LITE_ATTN_NORM_ROW;
+    const bool row = p.by_row;
     s.part[x] = p.side[x].part;
     s.out[x] = out[x];
     s.columns[x] = out[x] ? (row ? p.side[x].heads : 1) * p.head_dim : 0;

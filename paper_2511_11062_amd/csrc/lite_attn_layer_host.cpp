@@ -89,6 +89,7 @@ int log2_up(int x) {
 
 struct RotaryShape {
   int lanes, team_heads, near_heads, groups, row_lanes, sum_log, tokens, threads, shares;
+  Sums sums;
   int kinds;  // of workgroups of a batch entry
 };
 
@@ -104,17 +105,25 @@ RotaryShape rotary_shape(const lite_attn_rotary_desc_t& d, bool bwd, bool togeth
   s.team_heads = by_row ? most : std::min(most, std::max(1, 256 / s.lanes));
   s.groups = (most + s.team_heads - 1) / s.team_heads;
   s.row_lanes = s.team_heads * s.lanes;
-  s.sum_log = -1;
-  if (by_row && s.row_lanes <= 64) {
+  s.sum_log = 0;
+  if (d.norm == LITE_ATTN_NORM_NONE) {
+    s.sums = kSumNone;
+  } else if (by_row && s.row_lanes <= 64) {
+    s.sums = kSumLanes;
     s.sum_log = log2_up(s.row_lanes);
     s.row_lanes = 1 << s.sum_log;
-  } else if (!by_row && (s.lanes & (s.lanes - 1)) == 0) {
+  } else if (by_row) {
+    s.sums = kSumWaves;
+  } else if ((s.lanes & (s.lanes - 1)) == 0) {
+    s.sums = kSumLanes;
     s.sum_log = log2_up(s.lanes);
+  } else {
+    s.sums = kSumHeads;
   }
-  s.tokens = together && (!by_row || s.sum_log >= 0) ? std::max(1, std::min(256 / s.row_lanes, d.seqlen)) : 1;
+  s.tokens = together && s.sums != kSumWaves ? std::max(1, std::min(256 / s.row_lanes, d.seqlen)) : 1;
   s.threads = (s.tokens * s.row_lanes + 63) / 64 * 64;
   s.near_heads = s.tokens > 1 ? s.team_heads : std::min(s.team_heads, 64 % s.lanes ? 63 / s.lanes + 2 : 64 / s.lanes);
-  s.kinds = s.groups * (rotary_sides(d.norm, bwd) == 1 && d.heads_k ? 2 : 1);
+  s.kinds = s.groups * (rotary_sides(d.norm != LITE_ATTN_NORM_NONE, bwd) == 1 && d.heads_k ? 2 : 1);
   const int64_t bytes = (int64_t)s.tokens * s.team_heads * d.head_dim * size_of(d.dtype);
   s.shares = shares_of((int64_t)d.batch * s.kinds, (int)(((int64_t)d.seqlen + s.tokens - 1) / s.tokens), s.threads / 64,
                        bwd && d.norm != LITE_ATTN_NORM_NONE ? 2 * bytes : bytes);
@@ -172,7 +181,7 @@ int fill_rotary(const lite_attn_rotary_desc_t& d, const lite_attn_positions_t& a
   p->near_heads = s.near_heads;
   p->row_lanes = s.row_lanes;
   p->sum_log = s.sum_log;
-  p->norm = d.norm;
+  p->by_row = d.norm == LITE_ATTN_NORM_ROW;
   p->halves = d.halves;
   p->weight_dtype = d.weight_dtype;
   p->token_start = at.token_start;
@@ -243,6 +252,7 @@ int plan_rotary(const lite_attn_rotary_desc_t& d, const lite_attn_rotary_fwd_t& 
     p->shared_writes |= shares_lines(out[x], d);
     p->shared_reads |= p->shared_writes | shares_lines(in[x], d);
   }
+  l->sums = s.sums;
   return launch_of(d.batch, (int64_t)s.shares * s.kinds, s.threads, l);
 }
 
@@ -284,6 +294,7 @@ int plan_rotary(const lite_attn_rotary_desc_t& d, const lite_attn_rotary_bwd_t& 
     if (grads[x]) p->side[x].part = part;
     part += (size_t)d.batch * s.shares * rotary_part(d, s, x);
   }
+  l->sums = s.sums;
   return launch_of(d.batch, (int64_t)s.shares * s.kinds, s.threads, l);
 }
 

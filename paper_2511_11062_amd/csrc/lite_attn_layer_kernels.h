@@ -30,8 +30,11 @@ struct RotarySide {
   int heads;
 };
 
+// What a norm's sums go over: no norm; neighbouring lanes, a power of two of them; the lanes of a head, by way of LDS; all waves
+// of the workgroup.
+enum Sums { kSumNone, kSumLanes, kSumHeads, kSumWaves };
 // Of q and k, how many a workgroup takes.
-constexpr int rotary_sides(int norm, bool bwd) { return bwd && norm != LITE_ATTN_NORM_NONE ? 1 : 2; }
+constexpr int rotary_sides(bool normed, bool bwd) { return bwd && normed ? 1 : 2; }
 
 struct RotaryParams {
   RotarySide side[2];
@@ -48,8 +51,8 @@ struct RotaryParams {
   int groups;            // of as many heads
   int near_heads;        // heads that offsets from one place reach: the workgroup's or, if it takes one token, a wave's
   int row_lanes;         // threads of a token: of its heads, under NORM_ROW up to 64 rounded up to a power of two
-  int sum_log;           // sums go over 1 << sum_log neighbouring lanes; -1: over all waves (NORM_ROW), or by way of LDS
-  int norm, halves, weight_dtype;
+  int sum_log;           // kSumLanes: sums go over 1 << sum_log neighbouring lanes
+  int by_row, halves, weight_dtype;  // by_row: NORM_ROW
   int shared_reads, shared_writes;  // neighbouring tokens share lines of memory, of an input or a result; of a result
   int token_start, area, width, video;  // area = height * width, video = frames * area
   float eps;
@@ -78,6 +81,7 @@ struct ResidualParams {
 
 struct LayerLaunch {
   int threads, blocks;
+  Sums sums;  // rotary
 };
 
 // lite_attn_layer_host.cpp (no HIP calls): checks, and what a call launches
