@@ -694,25 +694,31 @@ __global__ __launch_bounds__(1024) void sum_rows_kernel(const RowSums p) {
 // ---- residual stream ---------------------------------------------------------------------------------------------------
 
 // The columns of a row that a thread holds: kEach in a row; four and four, where 32-bit entries are among them, so that the lanes
-// of an access of 16 bytes each lie side by side; of ragged rows (of a number of entries that kEach does not divide) one of each
-// `team`.  What lies behind the row reads as 0 and is not written.
-enum Spread { kEights, kFours, kOnes };
+// of an access of 16 bytes each lie side by side; one of each `team` in rows of fewer than eight.  Rows that are not whole pieces
+// (TAIL): the last piece is moved back until it ends with the row.  What it has in common with the one before it is read and
+// written by both, the same values, and counts in the other's sums only.  What lies behind the row reads as 0 and is not written.
+enum Spread { kEights, kFours, kEightsTail, kFoursTail, kOnes };
+constexpr bool has_tail(Spread s) { return s == kEightsTail || s == kFoursTail; }
+constexpr int piece_of(Spread s) { return s == kOnes ? 1 : s == kFours || s == kFoursTail ? 4 : 8; }
 template <Spread S>
 struct Columns {
   int thread, team, D;
-  __device__ __forceinline__ int at(int e) const {
-    return S == kOnes ? thread + e * team : S == kFours ? (e / 4 * team + thread) * 4 + e % 4 : thread * kEach + e;
+  // where the piece of entry e starts: its own place, and the one it is moved to
+  __device__ __forceinline__ int own(int e) const { return (e / piece_of(S) * team + thread) * piece_of(S); }
+  __device__ __forceinline__ int start(int e) const {
+    return has_tail(S) && own(e) < D ? min(own(e), D - piece_of(S)) : own(e);
   }
-  __device__ __forceinline__ bool has(int e) const { return at(S == kOnes ? e : S == kFours ? e / 4 * 4 : 0) < D; }
+  __device__ __forceinline__ int at(int e) const { return start(e) + e % piece_of(S); }
+  __device__ __forceinline__ bool has(int e) const { return has_tail(S) ? own(e) < D && at(e) >= own(e) : own(e) < D; }
 };
 template <class Kind, Spread S>
-constexpr int kRowAccesses = S == kOnes ? kEach : S == kFours ? 2 : Piece<Kind>::kSize / 2;  // loads or stores of a row
+constexpr int kRowAccesses = S == kOnes ? kEach : piece_of(S) == 4 ? 2 : Piece<Kind>::kSize / 2;  // loads or stores of a row
 template <Spread S, class Kind>
 __device__ __forceinline__ void load_row(Buffer from, const Columns<S>& col, Piece<Kind>& to) {
   if constexpr (S == kOnes) {
 #pragma unroll
     for (int e = 0; e < kEach; e += 2) to.load_two(e, from, col.at(e) * to.kSize, col.at(e + 1) * to.kSize);
-  } else if constexpr (S == kFours) {
+  } else if constexpr (piece_of(S) == 4) {
     to.load_run(0, from, col.at(0) * to.kSize);
     to.load_run(1, from, col.at(4) * to.kSize);
   } else {
@@ -726,7 +732,7 @@ __device__ __forceinline__ void store_row(Buffer to, const Columns<S>& col, cons
   if constexpr (S == kOnes) {
 #pragma unroll
     for (int e = 0; e < kEach; e += 2) out.store_two(e, to, col.at(e) * out.kSize, col.at(e + 1) * out.kSize);
-  } else if constexpr (S == kFours) {
+  } else if constexpr (piece_of(S) == 4) {
     out.store_run(0, to, col.at(0) * out.kSize);
     out.store_run(1, to, col.at(4) * out.kSize);
   } else {
@@ -814,7 +820,8 @@ __device__ __forceinline__ Stats row_stats(Team& team, const float* x, const Col
   if (kind == LITE_ATTN_NORM_LAYER) {
     float s = 0.f;
 #pragma unroll
-    for (int e = 0; e < kEach; ++e) s += x[e];  // (0 where the thread has no column)
+    for (int e = 0; e < kEach; ++e)
+      if (!has_tail(S) || col.has(e)) s += x[e];  // (0 where there is no column)
     mean = sum64(s) * counts.mine_inv;
   }
   float sq = 0.f;
@@ -1159,8 +1166,13 @@ void launch_residual_way(const ResidualParams& p, const LayerLaunch& l, bool bwd
 }
 template <class KindX, class KindY>
 void launch_residual_kind(const ResidualParams& p, const LayerLaunch& l, bool bwd, hipStream_t st) {
-  constexpr Spread kWhole = Piece<KindX>::kSize == 4 ? kFours : kEights;
-  p.D % kEach ? launch_residual_way<KindX, KindY, kOnes>(p, l, bwd, st) : launch_residual_way<KindX, KindY, kWhole>(p, l, bwd, st);
+  constexpr bool kWide = Piece<KindX>::kSize == 4;
+  if (p.D % kEach == 0)
+    launch_residual_way<KindX, KindY, kWide ? kFours : kEights>(p, l, bwd, st);
+  else if (p.D > kEach)
+    launch_residual_way<KindX, KindY, kWide ? kFoursTail : kEightsTail>(p, l, bwd, st);
+  else
+    launch_residual_way<KindX, KindY, kOnes>(p, l, bwd, st);
 }
 
 }  // namespace
