@@ -223,20 +223,30 @@ __device__ __forceinline__ void lds_barrier() {
   __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "workgroup", "local");
 }
 
-// Sums of two values over all waves of the workgroup; `mine` are a wave's own.  The two halves of `room` serve in turn: a wave
-// that is one sum ahead cannot overwrite what another still reads, as there is a barrier between.
+// What the waves of a workgroup tell each other: kCount pairs of values each.  The two halves of a room serve in turn: a wave that
+// is one exchange ahead cannot overwrite what another still reads, as there is a barrier between.
+template <int kCount>
 struct WaveRoom {
-  f32x2 v[2][kMaxTeam / 64];
+  f32x2 v[2][kCount][kMaxTeam / 64];
+  // This wave's values -> those of wave threadIdx.x % 16 (0 if there is none).
+  template <int kUsed>
+  __device__ __forceinline__ void exchange(int& turn, f32x2 (&x)[kUsed]) {
+    static_assert(kUsed <= kCount, "room for them");
+    if ((threadIdx.x & 63) == 0) {
+#pragma unroll
+      for (int i = 0; i < kUsed; ++i) v[turn][i][threadIdx.x >> 6] = x[i];
+    }
+    lds_barrier();
+    const int w = threadIdx.x & 15;
+    const bool there = w < (int)(blockDim.x >> 6);
+#pragma unroll
+    for (int i = 0; i < kUsed; ++i) {
+      x[i] = v[turn][i][w];
+      if (!there) x[i] = f32x2{0.f, 0.f};
+    }
+    turn ^= 1;
+  }
 };
-__device__ __forceinline__ void put_waves(WaveRoom* room, int turn, f32x2 mine) {
-  if ((threadIdx.x & 63) == 0) room->v[turn][threadIdx.x >> 6] = mine;
-}
-__device__ __forceinline__ f32x2 get_waves(const WaveRoom* room, int turn) {
-  const int w = threadIdx.x & 15;
-  f32x2 x = room->v[turn][w];
-  if (w >= (int)(blockDim.x >> 6)) x = f32x2{0.f, 0.f};
-  return x;
-}
 
 // ---- rotary positions --------------------------------------------------------------------------------------------------
 
@@ -341,7 +351,7 @@ __global__ __launch_bounds__(SUMS == kSumWaves ? kMaxTeam : 256) void rotary_ker
   constexpr int kSides = rotary_sides(kNormed, BWD);
   touch_arguments<sizeof(RotaryParams)>();
   __shared__ f32x2 angles[kAngles];
-  __shared__ WaveRoom room;
+  __shared__ WaveRoom<1> room;
   __shared__ f32x2 lane_sums[2][SUMS == kSumHeads ? 256 + 64 : 1];  // (threads of no head read on behind 256)
   const int tid = threadIdx.x;
   // Workgroups go to the XCDs in turn.  Where neighbouring tokens share lines, an XCD takes neighbouring shares, and its cache
@@ -512,20 +522,20 @@ __global__ __launch_bounds__(SUMS == kSumWaves ? kMaxTeam : 256) void rotary_ker
     } else if constexpr (SUMS == kSumWaves) {
       x[0] = sum64(x[0]);
       if constexpr (BWD) x[1] = sum64(x[1]);
-      put_waves(&room, turn, x);
-      lds_barrier();
-      x = get_waves(&room, turn);
-      x[0] = sum16(x[0]);
-      if constexpr (BWD) x[1] = sum16(x[1]);
+      f32x2 all[1] = {x};
+      room.exchange(turn, all);
+      x[0] = sum16(all[0][0]);
+      if constexpr (BWD) x[1] = sum16(all[0][1]);
+      return x;
     } else {
       lane_sums[turn][tid] = x;
       lds_barrier();
       const f32x2* const mine = &lane_sums[turn][tid - c];
       x = mine[0];
       for (int l = 1; l < p.lanes; ++l) x += mine[l];
+      turn ^= 1;
+      return x;
     }
-    turn ^= 1;
-    return x;
   };
   // A row; the next one is of `next_side`.
   auto do_row = [&](auto index, bool here, int next_side, bool there) {
@@ -765,47 +775,21 @@ __device__ __forceinline__ void load_mod(const Lines& l, int dtype, int b, int g
   load_params(l.data ? l.data + b * l.stride_b + g * l.stride_n : nullptr, dtype, col, to, missing);
 }
 
-// Sums over a row's team, the waves of the workgroup.
+// A row's team, the waves of the workgroup.
 struct Team {
   bool waves;  // more than one
   int turn;
-  WaveRoom* room;
-  // This wave's values -> those of wave threadIdx.x % 16 (0 if there is none).
-  __device__ __forceinline__ f32x2 exchange(f32x2 x) {
-    put_waves(room, turn, x);
-    lds_barrier();
-    x = get_waves(room, turn);
-    turn ^= 1;
-    return x;
+  WaveRoom<3>* room;
+  template <int kUsed>
+  __device__ __forceinline__ void exchange(f32x2 (&x)[kUsed]) {
+    if (waves) room->exchange(turn, x);
   }
-  __device__ __forceinline__ f32x2 sum(f32x2 x) {
-    x = f32x2{sum64(x[0]), sum64(x[1])};
-    if (!waves) return x;
-    x = exchange(x);
-    return f32x2{sum16(x[0]), sum16(x[1])};
-  }
+  __device__ __forceinline__ float total(float x) const { return waves ? sum16(x) : x; }  // of the waves' values
 };
 
-// Gradient through a norm: d -> rstd (d - mean(d) [LAYER] - n mean(d n)).
-template <Spread S>
-__device__ __forceinline__ void norm_back(Team& team, float* d, const float* n, float rstd, int kind, float inv_D,
-                                          const Columns<S>& col) {
-  f32x2 s = {0.f, 0.f};
-#pragma unroll
-  for (int e = 0; e < kEach; ++e) {
-    if (!col.has(e)) continue;
-    s[0] += d[e];
-    s[1] += d[e] * n[e];
-  }
-  s = team.sum(s);
-  const float mean = kind == LITE_ATTN_NORM_LAYER ? s[0] * inv_D : 0.f, pull = s[1] * inv_D;
-#pragma unroll
-  for (int e = 0; e < kEach; ++e) d[e] = rstd * (d[e] - mean - n[e] * pull);
-}
-
-// Mean (0 under RMS) and 1 / standard deviation of a row.  Under LAYER the squares are taken about the wave's own mean, and
-// those of the waves put together (squares about the row's mean = theirs + count * (their mean - the row's)^2): one exchange
-// between waves, and nothing cancels where the mean is large.  `counts`: entries of a row in this wave, and in wave
+// Mean (0 under RMS) and 1 / standard deviation of a row, from two values of each wave: its own mean, and its squares about that.
+// Those of the waves are put together by: squares about the row's mean = theirs + count * (their mean - the row's)^2.  So it takes
+// one exchange between waves, and nothing cancels where the mean is large.  Counts: entries of a row in this wave, and in wave
 // threadIdx.x % 16.
 struct Counts {
   float mine_inv, other;
@@ -814,8 +798,7 @@ struct Stats {
   float mean, rstd;
 };
 template <Spread S>
-__device__ __forceinline__ Stats row_stats(Team& team, const float* x, const Columns<S>& col, int kind, float eps, float inv_D,
-                                           const Counts& counts) {
+__device__ __forceinline__ f32x2 wave_stats(const float* x, const Columns<S>& col, int kind, const Counts& counts) {
   float mean = 0.f;
   if (kind == LITE_ATTN_NORM_LAYER) {
     float s = 0.f;
@@ -830,17 +813,28 @@ __device__ __forceinline__ Stats row_stats(Team& team, const float* x, const Col
     const float d = x[e] - mean;
     if (col.has(e)) sq += d * d;
   }
-  sq = sum64(sq);
-  if (team.waves) {
-    f32x2 w = team.exchange(f32x2{mean, sq});
-    if (kind == LITE_ATTN_NORM_LAYER) {
-      mean = sum16(w[0] * counts.other) * inv_D;
-      const float d = w[0] - mean;
-      w[1] += counts.other * d * d;
-    }
-    sq = sum16(w[1]);
+  return f32x2{mean, sum64(sq)};
+}
+__device__ __forceinline__ Stats row_stats(const Team& team, f32x2 w, int kind, float eps, float inv_D, const Counts& counts) {
+  float mean = w[0];
+  if (team.waves && kind == LITE_ATTN_NORM_LAYER) {
+    mean = sum16(w[0] * counts.other) * inv_D;
+    const float d = w[0] - mean;
+    w[1] += counts.other * d * d;
   }
-  return {mean, rsqrtf(sq * inv_D + eps)};
+  return {mean, rsqrtf(team.total(w[1]) * inv_D + eps)};
+}
+// Sums that the gradient d of a norm's result asks for, over this wave: of d, and of d (x - mean).
+template <Spread S>
+__device__ __forceinline__ f32x2 wave_dots(const float* d, const float* x, float mean, const Columns<S>& col) {
+  f32x2 s = {0.f, 0.f};
+#pragma unroll
+  for (int e = 0; e < kEach; ++e) {
+    if (!col.has(e)) continue;
+    s[0] += d[e];
+    s[1] += d[e] * (x[e] - mean);
+  }
+  return f32x2{sum64(s[0]), sum64(s[1])};
 }
 
 // The workgroup's share of the rows of a group.
@@ -872,8 +866,8 @@ __device__ __forceinline__ Counts count_columns(const ResidualParams& p, const C
 }
 
 template <class KindX, class KindY, Spread S>
-__global__ __launch_bounds__(kMaxTeam) void residual_fwd_kernel(const ResidualParams p) {
-  __shared__ WaveRoom room;
+__global__ __launch_bounds__(S == kOnes ? 64 : kMaxTeam) void residual_fwd_kernel(const ResidualParams p) {
+  __shared__ WaveRoom<3> room;
   __shared__ float in_waves[kMaxTeam / 64];
   touch_arguments<sizeof(ResidualParams)>();
   const Share share(p);
@@ -924,7 +918,9 @@ __global__ __launch_bounds__(kMaxTeam) void residual_fwd_kernel(const ResidualPa
       float y[kEach];
       py.unpack(y);
       if (p.post != LITE_ATTN_NORM_NONE) {
-        const Stats s = row_stats(team, y, col, p.post, p.post_eps, p.inv_D, counts);
+        f32x2 w[1] = {wave_stats(y, col, p.post, counts)};
+        team.exchange(w);
+        const Stats s = row_stats(team, w[0], p.post, p.post_eps, p.inv_D, counts);
 #pragma unroll
         for (int e = 0; e < kEach; ++e) y[e] = (y[e] - s.mean) * s.rstd;
       }
@@ -935,7 +931,9 @@ __global__ __launch_bounds__(kMaxTeam) void residual_fwd_kernel(const ResidualPa
     x_to.step();
     if (p.h.data) {
       if (p.pre != LITE_ATTN_NORM_NONE) {
-        const Stats s = row_stats(team, x, col, p.pre, p.pre_eps, p.inv_D, counts);
+        f32x2 w[1] = {wave_stats(x, col, p.pre, counts)};
+        team.exchange(w);
+        const Stats s = row_stats(team, w[0], p.pre, p.pre_eps, p.inv_D, counts);
 #pragma unroll
         for (int e = 0; e < kEach; ++e) x[e] = (x[e] - s.mean) * s.rstd;
       }
@@ -951,10 +949,12 @@ __global__ __launch_bounds__(kMaxTeam) void residual_fwd_kernel(const ResidualPa
 //   dx = dx_out + rstd (dn - mean(dn) [LAYER] - n mean(dn n))
 //   dy = the same of dp post_w, dp = alpha gate dx, with n_y = post(y)
 // and over the tokens of a row of modulation A = sum dh n, S = sum dh, C = sum dx n_y, from which all six gradients of the
-// parameters follow (group_sums_kernel): three sums in registers, where each gradient by itself would need six.
+// parameters follow (group_sums_kernel): three sums in registers, where each gradient by itself would need six.  The waves meet
+// once for x, with both rows' statistics and the sums of dn and of dn (x - the wave's mean), which those of the waves are put
+// together from like the squares, and once more for y: us at 2 x 3913 rows of 1111, four meetings -> two, 53.8 -> 47.
 template <class KindX, class KindY, Spread S>
-__global__ __launch_bounds__(kMaxTeam) void residual_bwd_kernel(const ResidualParams p) {
-  __shared__ WaveRoom room;
+__global__ __launch_bounds__(S == kOnes ? 64 : kMaxTeam) void residual_bwd_kernel(const ResidualParams p) {
+  __shared__ WaveRoom<3> room;
   __shared__ float in_waves[kMaxTeam / 64];
   touch_arguments<sizeof(ResidualParams)>();
   const Share share(p);
@@ -967,12 +967,14 @@ __global__ __launch_bounds__(kMaxTeam) void residual_bwd_kernel(const ResidualPa
   Walk dxo_in = share.walk(p.dxo, row_x), y_in = share.walk(p.y, row_y);
   Walk dx_to = share.walk(p.dx, row_x), dy_to = share.walk(p.dy, row_y);
   Piece<KindX> next_x, dxo;
-  Piece<KindY> next_dh, py;
+  Piece<KindY> next_dh, next_y;
   auto fetch_next = [&](bool there) {
     load_row(x_in.row_if(there), col, next_x);
     load_row(dh_in.row_if(there), col, next_dh);
+    load_row(y_in.row_if(there), col, next_y);
     x_in.step();
     dh_in.step();
+    y_in.step();
   };
   fetch_next(true);
   const Counts counts = count_columns(p, col, in_waves);
@@ -996,55 +998,70 @@ __global__ __launch_bounds__(kMaxTeam) void residual_bwd_kernel(const ResidualPa
   for (int n = share.n0; n < share.end; n += share.step) {
     // what the row needs first is asked for a row ahead, the rest now
     const Piece<KindX> px = next_x;
-    const Piece<KindY> pdh = next_dh;
+    const Piece<KindY> pdh = next_dh, py = next_y;
     load_row(dxo_in.row(), col, dxo);
-    load_row(y_in.row(), col, py);
     dxo_in.step();
-    y_in.step();
     fetch_next(n + share.step < share.end);
-    float dx[kEach];
-    if (p.dh.data) {
-      float x[kEach];
-      float rstd = 1.f;
-      px.unpack(x);
-      pdh.unpack(dx);
-      if (p.pre != LITE_ATTN_NORM_NONE) {
-        const Stats s = row_stats(team, x, col, p.pre, p.pre_eps, p.inv_D, counts);
-        rstd = s.rstd;
-#pragma unroll
-        for (int e = 0; e < kEach; ++e) x[e] = (x[e] - s.mean) * rstd;
-      }
-#pragma unroll
-      for (int e = 0; e < kEach; ++e) {
-        sum_a[e] += dx[e] * x[e];
-        sum_s[e] += dx[e];
-        dx[e] *= mul[e];
-      }
-      if (p.pre != LITE_ATTN_NORM_NONE) norm_back(team, dx, x, rstd, p.pre, p.inv_D, col);
-    } else {
-#pragma unroll
-      for (int e = 0; e < kEach; ++e) dx[e] = 0.f;
-    }
-    float y[kEach];
-    dxo.unpack(y);
-#pragma unroll
-    for (int e = 0; e < kEach; ++e) dx[e] += y[e];
-    store_row<KindX>(dx_to.row(), col, dx);
-    dx_to.step();
-    float rstd = 1.f;
+    const bool pre = p.dh.data && p.pre != LITE_ATTN_NORM_NONE, post = p.y.data && p.post != LITE_ATTN_NORM_NONE;
+    float dx[kEach], x[kEach], y[kEach];
+    px.unpack(x);
     py.unpack(y);
-    if (p.y.data && p.post != LITE_ATTN_NORM_NONE) {
-      const Stats s = row_stats(team, y, col, p.post, p.post_eps, p.inv_D, counts);
+    pdh.unpack(dx);  // (0 if there is no dh)
+#pragma unroll
+    for (int e = 0; e < kEach; ++e) {
+      sum_s[e] += dx[e];
+      if (!pre && p.dh.data) sum_a[e] += dx[e] * x[e];
+    }
+    float dh[kEach];
+#pragma unroll
+    for (int e = 0; e < kEach; ++e) {
+      dh[e] = dx[e];
+      dx[e] *= mul[e];
+    }
+    f32x2 w[3] = {};
+    if (pre) {
+      w[0] = wave_stats(x, col, p.pre, counts);
+      w[1] = wave_dots(dx, x, w[0][0], col);
+    }
+    if (post) w[2] = wave_stats(y, col, p.post, counts);
+    if (pre || post) team.exchange(w);
+    float rstd = 1.f;
+    if (post) {
+      const Stats s = row_stats(team, w[2], p.post, p.post_eps, p.inv_D, counts);
       rstd = s.rstd;
 #pragma unroll
       for (int e = 0; e < kEach; ++e) y[e] = (y[e] - s.mean) * rstd;
     }
+    if (pre) {
+      const Stats s = row_stats(team, w[0], p.pre, p.pre_eps, p.inv_D, counts);
+      const float mean = p.pre == LITE_ATTN_NORM_LAYER ? team.total(w[1][0]) * p.inv_D : 0.f;
+      const float pull = team.total(w[1][1] + (w[0][0] - s.mean) * w[1][0]) * s.rstd * p.inv_D;
+#pragma unroll
+      for (int e = 0; e < kEach; ++e) {
+        x[e] = (x[e] - s.mean) * s.rstd;
+        sum_a[e] += dh[e] * x[e];
+        dx[e] = s.rstd * (dx[e] - mean - x[e] * pull);
+      }
+    }
+    float more[kEach];
+    dxo.unpack(more);
+#pragma unroll
+    for (int e = 0; e < kEach; ++e) dx[e] += more[e];
+    store_row<KindX>(dx_to.row(), col, dx);
+    dx_to.step();
 #pragma unroll
     for (int e = 0; e < kEach; ++e) {
       sum_c[e] += dx[e] * y[e];
       dx[e] *= open[e];
     }
-    if (p.dy.data && p.post != LITE_ATTN_NORM_NONE) norm_back(team, dx, y, rstd, p.post, p.inv_D, col);
+    if (post && p.dy.data) {
+      f32x2 d[1] = {wave_dots(dx, y, 0.f, col)};
+      team.exchange(d);
+      const float mean = p.post == LITE_ATTN_NORM_LAYER ? team.total(d[0][0]) * p.inv_D : 0.f;
+      const float pull = team.total(d[0][1]) * p.inv_D;
+#pragma unroll
+      for (int e = 0; e < kEach; ++e) dx[e] = rstd * (dx[e] - mean - y[e] * pull);
+    }
     store_row<KindY>(dy_to.row(), col, dx);
     dy_to.step();
   }
