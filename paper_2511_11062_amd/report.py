@@ -15,12 +15,25 @@ import json
 import torch
 
 from . import inputs
+from . import layer
 from . import lite_attn as la
 
 
 # threshold sweep of the 12-head N=32760 sequence: found by a one-off sweep on the synthetic inputs, linear order;
 # skipped fraction at step 9: 0.299, 0.452, 0.603, 0.707 (eta_9: 0.13, 0.30, 0.71, 1.17)
 SWEEP_THRESHOLDS = {"wan1.3b_sweep": [-2.75, -1.5, -0.5, -0.1]}
+
+
+def turn_by_position(wl, q, k, theta=10000.0):
+    """q and k of a step, turned by their tokens' places in time, height and width as a model's layers have them: a third of a
+    head's pairs for each axis, text tokens left as they are."""
+    third = wl.head_dim // 6
+    freqs = torch.from_numpy(layer.lite_attn_rotary_freqs((wl.head_dim // 2 - 2 * third, third, third), theta).copy()).cuda()
+    desc = layer.make_rotary_desc(wl.batch, wl.seqlen, wl.heads, wl.heads, wl.head_dim, grid=wl.grid)
+    out = torch.empty_like(q), torch.empty_like(k)
+    views = [(t.data_ptr(), t.stride(0), t.stride(1), t.stride(2)) for t in (q, k, *out)]
+    layer.lite_attn_rotary_fwd(desc, *views, freqs.data_ptr(), hip_stream=torch.cuda.current_stream().cuda_stream)
+    return out
 
 
 def run_sequence(wl, data, thresholds, dense_out=None, diagonal_first=False, immediate=False):
@@ -67,14 +80,19 @@ def main():
     ap.add_argument("--immediate", action="store_true",
                     help="drop a fired tile in the call that marks it (Algorithm 2 literally) instead of from the next "
                          "call on")
+    ap.add_argument("--rotary", action="store_true",
+                    help="turn q and k by their tokens' positions in time, height and width before the attention call")
     args = ap.parse_args()
     wl = inputs.WORKLOADS[args.workload]
     steps = args.steps or wl.steps
     seq = inputs.DriftSequence(wl, "cuda:0")
     data = [next(seq) for _ in range(steps)]
+    if args.rotary:
+        data = [(*turn_by_position(wl, q, k), v) for q, k, v in data]
     thresholds = args.thresholds or SWEEP_THRESHOLDS.get(wl.name, [-4.0, -3.0, -2.0, -1.0])
     dense_out, dense_rows = run_sequence(wl, data, [-float("inf")] * steps)
     result = {"workload": wl.name, "steps": steps, "diagonal_first": args.diagonal_first, "immediate": args.immediate,
+              "rotary": args.rotary,
               "dense_ms": [r["attn_ms"] for r in dense_rows], "runs": []}
     for thr in thresholds:
         _, rows = run_sequence(wl, data, [thr] * steps, dense_out, args.diagonal_first, args.immediate)
