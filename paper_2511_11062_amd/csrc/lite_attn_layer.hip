@@ -713,13 +713,34 @@ constexpr int piece_of(Spread s) { return s == kOnes ? 1 : s == kFours || s == k
 template <Spread S>
 struct Columns {
   int thread, team, D;
+  // TAIL: 1 of entries that count in this thread's sums, else 0 (a mask for each would not fit the scalar registers); of pieces of
+  // four, where vector registers are short too, the first of each piece that counts
+  float weight[S == kEightsTail ? kEach : 1];
+  int from[2];
+  __device__ __forceinline__ Columns(int thread_, int team_, int D_) : thread(thread_), team(team_), D(D_) {
+    if constexpr (S == kEightsTail) {
+#pragma unroll
+      for (int e = 0; e < kEach; ++e) weight[e] = own(e) < D && at(e) >= own(e) ? 1.f : 0.f;
+    } else if constexpr (S == kFoursTail) {
+#pragma unroll
+      for (int run = 0; run < 2; ++run) from[run] = own(4 * run) < D ? own(4 * run) - start(4 * run) : 4;
+    }
+  }
   // where the piece of entry e starts: its own place, and the one it is moved to
   __device__ __forceinline__ int own(int e) const { return (e / piece_of(S) * team + thread) * piece_of(S); }
   __device__ __forceinline__ int start(int e) const {
     return has_tail(S) && own(e) < D ? min(own(e), D - piece_of(S)) : own(e);
   }
   __device__ __forceinline__ int at(int e) const { return start(e) + e % piece_of(S); }
-  __device__ __forceinline__ bool has(int e) const { return has_tail(S) ? own(e) < D && at(e) >= own(e) : own(e) < D; }
+  // x as entry e's part of a sum
+  __device__ __forceinline__ float part(int e, float x) const {
+    if constexpr (S == kEightsTail)
+      return x * weight[e];
+    else if constexpr (S == kFoursTail)
+      return afresh(from[e / 4]) <= e % 4 ? x : 0.f;
+    else
+      return own(e) < D ? x : 0.f;
+  }
 };
 template <class Kind, Spread S>
 constexpr int kRowAccesses = S == kOnes ? kEach : piece_of(S) == 4 ? 2 : Piece<Kind>::kSize / 2;  // loads or stores of a row
@@ -804,14 +825,14 @@ __device__ __forceinline__ f32x2 wave_stats(const float* x, const Columns<S>& co
     float s = 0.f;
 #pragma unroll
     for (int e = 0; e < kEach; ++e)
-      if (!has_tail(S) || col.has(e)) s += x[e];  // (0 where there is no column)
+      s += has_tail(S) ? col.part(e, x[e]) : x[e];  // (0 where there is no column)
     mean = sum64(s) * counts.mine_inv;
   }
   float sq = 0.f;
 #pragma unroll
   for (int e = 0; e < kEach; ++e) {
     const float d = x[e] - mean;
-    if (col.has(e)) sq += d * d;
+    sq += d * col.part(e, d);
   }
   return f32x2{mean, sum64(sq)};
 }
@@ -830,9 +851,9 @@ __device__ __forceinline__ f32x2 wave_dots(const float* d, const float* x, float
   f32x2 s = {0.f, 0.f};
 #pragma unroll
   for (int e = 0; e < kEach; ++e) {
-    if (!col.has(e)) continue;
-    s[0] += d[e];
-    s[1] += d[e] * (x[e] - mean);
+    const float t = col.part(e, d[e]);
+    s[0] += t;
+    s[1] += t * (x[e] - mean);
   }
   return f32x2{sum64(s[0]), sum64(s[1])};
 }
@@ -857,7 +878,7 @@ template <Spread S>
 __device__ __forceinline__ Counts count_columns(const ResidualParams& p, const Columns<S>& col, float* in_waves) {
   float mine = 0.f;
 #pragma unroll
-  for (int e = 0; e < kEach; ++e) mine += col.has(e) ? 1.f : 0.f;
+  for (int e = 0; e < kEach; ++e) mine += col.part(e, 1.f);
   mine = sum64(mine);
   if ((threadIdx.x & 63) == 0) in_waves[threadIdx.x >> 6] = mine;
   lds_barrier();
@@ -872,7 +893,7 @@ __global__ __launch_bounds__(S == kOnes ? 64 : kMaxTeam) void residual_fwd_kerne
   touch_arguments<sizeof(ResidualParams)>();
   const Share share(p);
   if (share.n0 >= share.end) return;  // (a group of fewer rows than shares)
-  const Columns<S> col = {(int)threadIdx.x, (int)blockDim.x, p.D};
+  const Columns<S> col((int)threadIdx.x, (int)blockDim.x, p.D);
   Team team = {blockDim.x > 64, 0, &room};
   const int row_x = p.D * Piece<KindX>::kSize, row_y = p.D * Piece<KindY>::kSize;
 
@@ -959,7 +980,7 @@ __global__ __launch_bounds__(S == kOnes ? 64 : kMaxTeam) void residual_bwd_kerne
   touch_arguments<sizeof(ResidualParams)>();
   const Share share(p);
   if (share.n0 >= share.end) return;  // (a group of fewer rows than shares)
-  const Columns<S> col = {(int)threadIdx.x, (int)blockDim.x, p.D};
+  const Columns<S> col((int)threadIdx.x, (int)blockDim.x, p.D);
   Team team = {blockDim.x > 64, 0, &room};
   const int row_x = p.D * Piece<KindX>::kSize, row_y = p.D * Piece<KindY>::kSize;
 
