@@ -61,15 +61,15 @@ bool good_vector(const T* p, int dtype) {
 }
 bool good_grad(const float* p) { return ((uintptr_t)p & 3) == 0; }
 
-// Shares that each of `kinds` kinds of rows is dealt to, at most `rows` (of a kind).  A workgroup of `waves` waves has a row of
-// `bytes` asked for at any time.  Memory gives most when 18 KB are asked for on each CU, in whole workgroups for each CU; more
-// of them get into each other's way.  us at 256 / 512 / 768 / 1024 / 1280 / 1536 workgroups: forwards 32760 x 1536, 9 KB a row,
-// 114 / 104 / 111 / 111 / 113 / 114, backwards, 18 KB, 159 / 167 / 185 / 188 / 199 / 199, 75600 x 5120, 20 KB, 514 / 564 / 555 / 592
-// / 614 / 607, rotary of 12 heads, 3 KB, 167 / 109 / 87 / 82 / 77 / 79, backwards, 6 KB, 220 / 140 / 121 / 121 / 121 / 123.  Kinds
-// that do not go evenly into that are dealt to four times as many, to be taken as CUs get free.
-int shares_of(int64_t kinds, int rows, int waves, int64_t bytes) {
-  const int64_t per_cu = std::max<int64_t>(1, std::min<int64_t>((18432 + bytes - 1) / bytes, 32 / waves));
-  const int64_t side_by_side = kCUs * per_cu;
+// Shares that each of `kinds` kinds of rows is dealt to, at most `rows` (of a kind), in workgroups of `waves` waves, `per_cu` of
+// them on a CU.  A workgroup has a row asked for at any time, and memory gives most when some 15 to 18 KB are asked for on each
+// CU, in whole workgroups for each CU: more of them get into each other's way, fewer do not keep it busy.  us at 256 / 512 / 768 /
+// 1024 / 1280 / 1536 workgroups: forwards 32760 x 1536, 9 KB a row, 114 / 104 / 111 / 111 / 113 / 114, 60000 x 1111, 4 KB, - / - / 108
+// / 115 / 124 / 127, 75600 x 5120, 20 KB, 514 / 564 / 555 / 592 / 614 / 607, backwards 32760 x 1536, 18 KB, 158 / 169 / 189 / 191 / 198
+// / 207, 12 KB, 149 / 119 / 128 / 136 / 148 / 154, rotary of 12 heads, 3 KB, 167 / 109 / 87 / 83 / 81 / 81, backwards, 6 KB, 220 / 138 /
+// 116 / 121 / 119 / 118.  Kinds that do not go evenly into that are dealt to four times as many, to be taken as CUs get free.
+int shares_of(int64_t kinds, int rows, int waves, int64_t per_cu) {
+  const int64_t side_by_side = kCUs * std::max<int64_t>(1, std::min<int64_t>(per_cu, 32 / waves));
   const int64_t shares = kinds * 4 <= side_by_side ? side_by_side / kinds : (4 * side_by_side + kinds - 1) / kinds;
   return (int)std::max<int64_t>(1, std::min<int64_t>(rows, shares));
 }
@@ -124,9 +124,10 @@ RotaryShape rotary_shape(const lite_attn_rotary_desc_t& d, bool bwd, bool togeth
   s.threads = (s.tokens * s.row_lanes + 63) / 64 * 64;
   s.near_heads = s.tokens > 1 ? s.team_heads : std::min(s.team_heads, 64 % s.lanes ? 63 / s.lanes + 2 : 64 / s.lanes);
   s.kinds = s.groups * (rotary_sides(d.norm != LITE_ATTN_NORM_NONE, bwd) == 1 && d.heads_k ? 2 : 1);
-  const int64_t bytes = (int64_t)s.tokens * s.team_heads * d.head_dim * size_of(d.dtype);
+  const int64_t bytes = (int64_t)s.tokens * s.team_heads * d.head_dim * size_of(d.dtype) *
+                        (bwd && d.norm != LITE_ATTN_NORM_NONE ? 2 : 1);
   s.shares = shares_of((int64_t)d.batch * s.kinds, (int)(((int64_t)d.seqlen + s.tokens - 1) / s.tokens), s.threads / 64,
-                       bwd && d.norm != LITE_ATTN_NORM_NONE ? 2 * bytes : bytes);
+                       (18432 + bytes - 1) / bytes);
   return s;
 }
 
@@ -309,11 +310,16 @@ int groups_of(const lite_attn_residual_desc_t& d) {
 }
 
 // A workgroup takes a row of `dim` entries, kEach in a thread, and rows of one group (tokens that share a row of modulation).
+// Backwards through a norm of y, whose sums come one after the other, a row takes longer, and one more workgroup on a CU pays (us
+// at 60000 x 1112, three -> four 207 -> 192; not in place of a single one, at 40000 x 5120 461 -> 480).
 ResidualShape residual_shape(const lite_attn_residual_desc_t& d, bool bwd) {
   ResidualShape s;
   s.threads = (d.dim + 64 * kEach - 1) / (64 * kEach) * 64;
+  const int64_t bytes = (int64_t)d.dim * (size_of(d.dtype) + size_of(d.stream_dtype));
+  int64_t per_cu = bwd ? (18432 + 2 * bytes - 1) / (2 * bytes) : (14848 + bytes / 2) / bytes;
+  if (bwd && d.post_norm != LITE_ATTN_NORM_NONE && per_cu > 1) ++per_cu;
   s.shares = shares_of(std::max<int64_t>(1, (int64_t)d.batch * groups_of(d)), std::min(d.tokens_per_mod, d.seqlen),
-                       s.threads / 64, (int64_t)d.dim * (size_of(d.dtype) + size_of(d.stream_dtype)) * (bwd ? 2 : 1));
+                       s.threads / 64, per_cu);
   return s;
 }
 
