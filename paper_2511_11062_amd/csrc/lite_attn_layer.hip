@@ -805,6 +805,12 @@ struct Team {
   __device__ __forceinline__ void exchange(f32x2 (&x)[kUsed]) {
     if (waves) room->exchange(turn, x);
   }
+  // A row may be worked on in place, and two waves may hold the same entries of it (TAIL): all of them are asked for before the
+  // waves meet in the row, and stored after that.  Where no norm makes them exchange anything, they meet here.
+  template <Spread S>
+  __device__ __forceinline__ void meet(bool exchanged) const {
+    if (has_tail(S) && waves && !exchanged) lds_barrier();
+  }
   __device__ __forceinline__ float total(float x) const { return waves ? sum16(x) : x; }  // of the waves' values
 };
 
@@ -933,12 +939,14 @@ __global__ __launch_bounds__(S == kOnes ? 64 : kMaxTeam) void residual_fwd_kerne
     const Piece<KindX> px = next_x;
     const Piece<KindY> py = next_y;
     fetch_next(n + share.step < share.end);
+    const bool post = p.y.data && p.post != LITE_ATTN_NORM_NONE, pre = p.h.data && p.pre != LITE_ATTN_NORM_NONE;
+    team.meet<S>(pre || post);
     float x[kEach];
     px.unpack(x);
     if (p.y.data) {
       float y[kEach];
       py.unpack(y);
-      if (p.post != LITE_ATTN_NORM_NONE) {
+      if (post) {
         f32x2 w[1] = {wave_stats(y, col, p.post, counts)};
         team.exchange(w);
         const Stats s = row_stats(team, w[0], p.post, p.post_eps, p.inv_D, counts);
@@ -951,7 +959,7 @@ __global__ __launch_bounds__(S == kOnes ? 64 : kMaxTeam) void residual_fwd_kerne
     store_row<KindX>(x_to.row(), col, x);
     x_to.step();
     if (p.h.data) {
-      if (p.pre != LITE_ATTN_NORM_NONE) {
+      if (pre) {
         f32x2 w[1] = {wave_stats(x, col, p.pre, counts)};
         team.exchange(w);
         const Stats s = row_stats(team, w[0], p.pre, p.pre_eps, p.inv_D, counts);
@@ -1024,6 +1032,7 @@ __global__ __launch_bounds__(S == kOnes ? 64 : kMaxTeam) void residual_bwd_kerne
     dxo_in.step();
     fetch_next(n + share.step < share.end);
     const bool pre = p.dh.data && p.pre != LITE_ATTN_NORM_NONE, post = p.y.data && p.post != LITE_ATTN_NORM_NONE;
+    team.meet<S>(pre || post);
     float dx[kEach], x[kEach], y[kEach];
     px.unpack(x);
     py.unpack(y);

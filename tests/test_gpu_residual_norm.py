@@ -322,6 +322,20 @@ def test_in_place():
     assert torch.equal(got[0], want[0]) and torch.equal(got[1], want[1])
 
 
+@pytest.mark.parametrize("dtype,stream", [("bf16", "bf16"), ("bf16", "f32"), ("f32", "f32")])
+@pytest.mark.parametrize("dim", [513, 517, 1025, 1541, 7681])
+def test_in_place_across_waves(dim, dtype, stream):
+    """Rows that end in entries held by two waves, and no norm that would make the waves wait for each other."""
+    c = Case(n=3000 if dim < 8000 else 700, dim=dim, dtype=dtype, stream=stream, pre="none")
+    dh, dxo = c.gradients()
+    wdx, wdy, wd = c.backward(dh, dxo)
+    dx, dy, d = c.backward(dh, dxo, dx=dxo, dy=dh)
+    assert torch.equal(dx, wdx) and torch.equal(dy, wdy) and all(torch.equal(d[k], wd[k]) for k in ("gate", "scale"))
+    want = c.forward()
+    got = c.forward(x_out=c.x, h=c.y)
+    assert torch.equal(got[0], want[0]) and torch.equal(got[1], want[1])
+
+
 def test_no_tokens():
     c = Case(batch=2, n=0, dim=64, weights=True)
     c.forward()
