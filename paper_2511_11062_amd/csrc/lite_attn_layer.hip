@@ -713,14 +713,18 @@ constexpr int piece_of(Spread s) { return s == kOnes ? 1 : s == kFours || s == k
 template <Spread S>
 struct Columns {
   int thread, team, D;
-  // TAIL: 1 of entries that count in this thread's sums, else 0 (a mask for each would not fit the scalar registers); of pieces of
-  // four, where vector registers are short too, the first of each piece that counts
-  float weight[S == kEightsTail ? kEach : 1];
+  // TAIL, which entries count in this thread's sums: all bits of them, or none (a mask over lanes for each would not fit the
+  // scalar registers, and a factor of 0 would make NaN of an infinity that counts elsewhere); of pieces of four, where vector
+  // registers are short too, the first of each piece that counts
+  uint32_t keep[S == kEightsTail ? kEach : 1];
   int from[2];
   __device__ __forceinline__ Columns(int thread_, int team_, int D_) : thread(thread_), team(team_), D(D_) {
     if constexpr (S == kEightsTail) {
 #pragma unroll
-      for (int e = 0; e < kEach; ++e) weight[e] = own(e) < D && at(e) >= own(e) ? 1.f : 0.f;
+      for (int e = 0; e < kEach; ++e) {
+        keep[e] = own(e) < D && at(e) >= own(e) ? 0xffffffffu : 0u;
+        asm volatile("" : "+v"(keep[e]));  // (or the compiler makes masks over lanes of them)
+      }
     } else if constexpr (S == kFoursTail) {
 #pragma unroll
       for (int run = 0; run < 2; ++run) from[run] = own(4 * run) < D ? own(4 * run) - start(4 * run) : 4;
@@ -735,7 +739,7 @@ struct Columns {
   // x as entry e's part of a sum
   __device__ __forceinline__ float part(int e, float x) const {
     if constexpr (S == kEightsTail)
-      return x * weight[e];
+      return __uint_as_float(__float_as_uint(x) & keep[e]);
     else if constexpr (S == kFoursTail)
       return afresh(from[e / 4]) <= e % 4 ? x : 0.f;
     else
@@ -837,8 +841,8 @@ __device__ __forceinline__ f32x2 wave_stats(const float* x, const Columns<S>& co
   float sq = 0.f;
 #pragma unroll
   for (int e = 0; e < kEach; ++e) {
-    const float d = x[e] - mean;
-    sq += d * col.part(e, d);
+    const float d = col.part(e, x[e] - mean);
+    sq += d * d;
   }
   return f32x2{mean, sum64(sq)};
 }
@@ -859,7 +863,7 @@ __device__ __forceinline__ f32x2 wave_dots(const float* d, const float* x, float
   for (int e = 0; e < kEach; ++e) {
     const float t = col.part(e, d[e]);
     s[0] += t;
-    s[1] += t * (x[e] - mean);
+    s[1] += t * (has_tail(S) ? col.part(e, x[e] - mean) : x[e] - mean);
   }
   return f32x2{sum64(s[0]), sum64(s[1])};
 }

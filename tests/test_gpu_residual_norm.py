@@ -355,6 +355,23 @@ def test_infinities_stay_with_their_token():
     assert torch.isinf(x_out[0, 3, 5])
 
 
+@pytest.mark.parametrize("dtype,stream", [("bf16", "bf16"), ("bf16", "f32"), ("f16", "f16"), ("f32", "f32")])
+@pytest.mark.parametrize("dim", [13, 519, 1111, 1541])
+def test_infinity_in_a_rows_last_entries(dim, dtype, stream):
+    """Under RMS an infinity makes NaN of itself and 0 of the row's other entries, wherever it stands."""
+    for column in range(dim - 9, dim):
+        c = Case(n=3, dim=dim, dtype=dtype, stream=stream, pre="rms", mods=False)
+        c.x[0, 1, column] = float("inf")
+        c.y.zero_()
+        h = c.forward()[1][0, 1]
+        others = [x for x in range(dim) if x != column]
+        assert torch.isnan(h[column]) and (h[others] == 0).all(), column
+        # backwards the mean of dn n makes NaN of the whole row, and of no other
+        dh, dxo = c.gradients()
+        dx = c.backward(dh, dxo)[0]
+        assert torch.isfinite(dx[0, [0, 2]]).all() and torch.isnan(dx[0, 1]).all()
+
+
 def test_rows_beyond_4_gib():
     c = Case(n=4, dim=256, dtype="bf16", stream="bf16")
     want = c.forward()
