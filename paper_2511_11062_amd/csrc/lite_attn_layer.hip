@@ -537,6 +537,16 @@ __global__ __launch_bounds__(SUMS == kSumWaves ? kMaxTeam : 256) void rotary_ker
       return x;
     }
   };
+  // Entries that are not turned stay what they are: a turn by 0 would make NaN of an entry beside an infinite one.
+  auto not_turned = [&](const float* xa, const float* xb, float* ra, float* rb) {
+    if (2 * P == p.head_dim) return;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      const bool turned = 4 * afresh(c) + e < P;
+      ra[e] = turned ? ra[e] : xa[e];
+      rb[e] = turned ? rb[e] : xb[e];
+    }
+  };
   // A row; the next one is of `next_side`.
   auto do_row = [&](auto index, bool here, int next_side, bool there) {
     constexpr int side = decltype(index)::value;
@@ -567,6 +577,7 @@ __global__ __launch_bounds__(SUMS == kSumWaves ? kMaxTeam : 256) void rotary_ker
         ra[e] = xa[e] * ca[e] - xb[e] * sa[e];
         rb[e] = xa[e] * sa[e] + xb[e] * ca[e];
       }
+      not_turned(xa, xb, ra, rb);
       store(side, out[side], here, ra, rb);
     } else {
       float ga[4], gb[4], za[4], zb[4];
@@ -576,6 +587,7 @@ __global__ __launch_bounds__(SUMS == kSumWaves ? kMaxTeam : 256) void rotary_ker
         za[e] = ga[e] * ca[e] + gb[e] * sa[e];
         zb[e] = gb[e] * ca[e] - ga[e] * sa[e];
       }
+      not_turned(ga, gb, za, zb);
       if constexpr (kNormed) {
         unpack(x, xa, xb);
         float sq = 0.f, dot = 0.f;

@@ -278,6 +278,25 @@ def test_infinities_stay_with_their_token():
     assert torch.isnan(got[0, 1, 5, 7]) and torch.isnan(got[0, :, 9]).all()
 
 
+@pytest.mark.parametrize("d,pairs", [(128, 40), (72, 30), (64, 0), (20, 7)])
+@pytest.mark.parametrize("halves", [False, True])
+def test_entries_that_are_not_turned_stand_alone(d, pairs, halves):
+    c = Case(heads=(3, 2), d=d, pairs=pairs, grid=(2, 3, 4), halves=halves)
+    grads = c.gradients()
+    want, wdq = c.forward()[0].clone(), c.backward(grads)[0].clone()
+    for column in range(2 * pairs, d, 5):
+        for bad in (float("inf"), float("nan")):
+            kept = c.q[0, 1, 7, column].clone(), grads[0][0, 1, 7, column].clone()
+            c.q[0, 1, 7, column] = grads[0][0, 1, 7, column] = bad
+            got, dq = c.forward()[0], c.backward(grads)[0]
+            for new, old in ((got, want), (dq, wdq)):
+                assert torch.equal(torch.isfinite(new), torch.ones_like(new, dtype=torch.bool).index_put_(
+                    tuple(torch.tensor([x], device="cuda") for x in (0, 1, 7, column)), torch.tensor(False, device="cuda")))
+                new[0, 1, 7, column] = old[0, 1, 7, column]
+                assert torch.equal(new, old)
+            c.q[0, 1, 7, column], grads[0][0, 1, 7, column] = kept
+
+
 def test_rows_beyond_4_gib():
     """A tensor whose tokens lie more than 2^32 bytes and 2^31 elements apart from its start."""
     c = Case(heads=(2, 2), d=64, grid=(1, 2, 2), norm="head")
