@@ -1121,32 +1121,34 @@ __global__ __launch_bounds__(S == kOnes ? 64 : kMaxTeam) void residual_bwd_kerne
   store_row<F32>(sums.row(), col, sum_c);
 }
 
-// Sums of a row of modulation: its shares' sums in order, each of the waves an equal part of them, and what follows from them.
+// Sums of a row of modulation: its shares' sums in order, kColumns threads an equal part of them, and what follows from them.
+// If the group is the only one, its parts of the weights' gradients are these gradients.
+template <int kColumns>  // that a workgroup takes
 __global__ __launch_bounds__(1024) void group_sums_kernel(const ResidualParams p, int all_groups) {
-  __shared__ float sums[16][3][64];
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, waves = blockDim.x >> 6;
-  const int column = blockIdx.y * 64 + lane;
+  __shared__ float sums[1024 / kColumns][3][kColumns];
+  const int lane = threadIdx.x % kColumns, part = threadIdx.x / kColumns, parts = blockDim.x / kColumns;
+  const int column = blockIdx.y * kColumns + lane;
   const size_t D = p.D;
   for (int group = blockIdx.x; group < all_groups; group += gridDim.x) {
     const int b = group / p.groups, g = group - b * p.groups;
     const int shares = min(p.shares, min(p.N, (g + 1) * p.per_mod) - g * p.per_mod);
-    const int from = part_start(shares, waves, wave), to = part_start(shares, waves, wave + 1);
+    const int from = part_start(shares, parts, part), to = part_start(shares, parts, part + 1);
     float a = 0.f, s = 0.f, c = 0.f;
     if (column < p.D) {
-      const float* part = p.part + ((size_t)group * p.shares + from) * 3 * D + column;
+      const float* at = p.part + ((size_t)group * p.shares + from) * 3 * D + column;
 #pragma unroll 4
-      for (int x = from; x < to; ++x, part += 3 * D) {
-        a += part[0];
-        s += part[D];
-        c += part[2 * D];
+      for (int x = from; x < to; ++x, at += 3 * D) {
+        a += at[0];
+        s += at[D];
+        c += at[2 * D];
       }
     }
-    sums[wave][0][lane] = a;
-    sums[wave][1][lane] = s;
-    sums[wave][2][lane] = c;
+    sums[part][0][lane] = a;
+    sums[part][1][lane] = s;
+    sums[part][2][lane] = c;
     __syncthreads();
-    if (wave == 0 && column < p.D) {
-      for (int w = 1; w < waves; ++w) {
+    if (part == 0 && column < p.D) {
+      for (int w = 1; w < parts; ++w) {
         a += sums[w][0][lane];
         s += sums[w][1][lane];
         c += sums[w][2][lane];
@@ -1155,20 +1157,19 @@ __global__ __launch_bounds__(1024) void group_sums_kernel(const ResidualParams p
       const size_t at = (size_t)group * D + column;
       const float post_w = p.post_w ? load_param(p.post_w, d, column) : 1.f;
       const float pre_w = p.pre_w ? load_param(p.pre_w, d, column) : 1.f;
-      const float pre_b = p.pre_b ? load_param(p.pre_b, d, column) : 0.f;
       auto mod = [&](const Lines& l, float missing) {
         return l.data ? load_param(l.data + b * l.stride_b + g * l.stride_n, d, column) : missing;
       };
       const float gate = mod(p.gate, 1.f), open = 1.f + mod(p.scale, 0.f);
       if (p.dgate) p.dgate[at] = p.alpha * post_w * c;
-      if (p.dscale) p.dscale[at] = pre_w * a + pre_b * s;
+      if (p.dscale) p.dscale[at] = pre_w * a + (p.pre_b ? load_param(p.pre_b, d, column) * s : 0.f);
       if (p.dshift) p.dshift[at] = s;
-      if (p.dpre_w || p.dpre_b || p.dpost_w) {
-        float* out = p.group_sums + (size_t)group * 3 * D + column;
-        out[0] = open * a;
-        out[D] = open * s;
-        out[2 * D] = p.alpha * gate * c;
-      }
+      const bool only = all_groups == 1;
+      float* const to_w[3] = {p.dpre_w, p.dpre_b, p.dpost_w};
+      const float w[3] = {open * a, open * s, p.alpha * gate * c};
+#pragma unroll
+      for (int x = 0; x < 3; ++x)
+        if (to_w[x]) (only ? to_w[x] : p.group_sums + ((size_t)group * 3 + x) * D)[column] = w[x];
     }
     __syncthreads();
   }
@@ -1286,15 +1287,22 @@ hipError_t launch_residual(const ResidualParams& p, const LayerLaunch& l, int dt
 
 hipError_t launch_residual_sums(const ResidualParams& p, hipStream_t st) {
   const int64_t groups = (int64_t)p.batch * p.groups;
-  const unsigned columns = (unsigned)(p.D + 63) / 64;
   if (groups > 0) {
     const int waves = p.shares < 2 ? 1 : p.shares < 32 ? 4 : 16;
-    const dim3 grid((unsigned)(groups < 65536 ? groups : 65536), columns);
-    group_sums_kernel<<<grid, 64 * waves, 0, st>>>(p, (int)groups);
+    // Few workgroups of 64 columns do not get the shares' sums in fast enough: us at 200000 rows of 128, 64 -> 32 columns 155 ->
+    // 139, 60000 of 1111 214 -> 207, 2 x 1000 of 1536 21.0 -> 20.5; but 8 groups of 1111 51.6 -> 55, 21 of 1536 173 -> 184.
+    const bool few = groups * ((p.D + 63) / 64) < 64;
+    const int columns = few ? 32 : 64;
+    const dim3 grid((unsigned)(groups < 65536 ? groups : 65536), (unsigned)((p.D + columns - 1) / columns));
+    if (few)
+      group_sums_kernel<32><<<grid, 64 * waves, 0, st>>>(p, (int)groups);
+    else
+      group_sums_kernel<64><<<grid, 64 * waves, 0, st>>>(p, (int)groups);
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
   }
-  if (p.dpre_w || p.dpre_b || p.dpost_w) weight_sums_kernel<<<dim3(columns, 3), 1024, 0, st>>>(p, (int)groups);
+  if (groups != 1 && (p.dpre_w || p.dpre_b || p.dpost_w))
+    weight_sums_kernel<<<dim3((unsigned)(p.D + 63) / 64, 3), 1024, 0, st>>>(p, (int)groups);
   return hipGetLastError();
 }
 

@@ -372,6 +372,17 @@ def test_infinity_in_a_rows_last_entries(dim, dtype, stream):
         assert torch.isfinite(dx[0, [0, 2]]).all() and torch.isnan(dx[0, 1]).all()
 
 
+def test_infinite_gradient_without_a_bias():
+    """The gradient of scale has a term of the bias; if there is none, no infinity is multiplied by its zero."""
+    c = Case(batch=2, n=9, dim=72, per=4, pre="rms")
+    dh, dxo = c.gradients()
+    dh[0, 5, 11] = float("inf")
+    dscale = c.backward(dh, dxo)[2]["scale"]
+    assert torch.isinf(dscale[0, 1, 11])
+    dscale[0, 1, 11] = 0.0
+    assert torch.isfinite(dscale).all()
+
+
 def test_rows_beyond_4_gib():
     c = Case(n=4, dim=256, dtype="bf16", stream="bf16")
     want = c.forward()
