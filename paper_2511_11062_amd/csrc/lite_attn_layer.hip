@@ -7,10 +7,17 @@
 //   sum_rows_kernel, group_sums_kernel, weight_sums_kernel : the shares' sums, in one fixed order
 //
 // All of them move some bytes for each of a few operations: they are bound by memory, and everything here serves to keep
-// enough bytes in flight and to do nothing twice.  A row is read once: its entries stay in the registers of a team of threads,
-// eight each, until its statistics are known.  A team takes a share of consecutive rows, asks for the next row before it works
-// on this one, and keeps what belongs to its columns -- weights, gate, scale, shift, sums over tokens -- in registers all the
-// while.  Sums over a row go through DPP inside a wave and once through LDS between waves.
+// enough bytes in flight and to do nothing twice.  A row is read once: its entries stay in the registers of a workgroup, eight
+// in a thread, until its statistics are known.  A workgroup takes every so many-th row, asks for its next one before it works on
+// this one, and keeps what belongs to its columns -- weights, gate, scale, shift, sums over tokens -- in registers all the while.
+// Sums over a row go through DPP inside a wave and once through LDS between waves.  Bytes that have to move, us and TB/s, where a
+// sum of two large tensors reaches 6.2 TB/s:
+//   rotary     40 heads of 128, 75600 tokens, norm over the token             3097 MB  655  4.7
+//              12 heads, 32760 tokens                                          402 MB   82  4.9
+//              the same backwards                                              604 MB  117  5.2
+//   residual   75600 x 5120, both norms, a row of modulation for 3600 tokens  3097 MB  606  5.1
+//              32760 x 1536, stream in 32 bits                                 604 MB  104  5.8
+//              the same backwards                                              906 MB  157  5.8
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 
@@ -32,14 +39,18 @@ typedef _Float16 f16x2 __attribute__((ext_vector_type(2)));
 // Element types: two of them as they lie in a word of memory (F32: one), and the word of two values, each rounded once.
 struct Bf16 {
   typedef __bf16 type;
-  static __device__ __forceinline__ f32x2 widen(uint32_t w) { return f32x2{__uint_as_float(w << 16), __uint_as_float(w & 0xffff0000u)}; }
+  static __device__ __forceinline__ f32x2 widen(uint32_t w) {
+    return f32x2{__uint_as_float(w << 16), __uint_as_float(w & 0xffff0000u)};
+  }
   static __device__ __forceinline__ uint32_t narrow(float a, float b) {
     return __builtin_bit_cast(uint32_t, __builtin_convertvector(f32x2{a, b}, bf16x2));
   }
 };
 struct F16 {
   typedef _Float16 type;
-  static __device__ __forceinline__ f32x2 widen(uint32_t w) { return __builtin_convertvector(__builtin_bit_cast(f16x2, w), f32x2); }
+  static __device__ __forceinline__ f32x2 widen(uint32_t w) {
+    return __builtin_convertvector(__builtin_bit_cast(f16x2, w), f32x2);
+  }
   static __device__ __forceinline__ uint32_t narrow(float a, float b) {
     return __builtin_bit_cast(uint32_t, __builtin_convertvector(f32x2{a, b}, f16x2));
   }
@@ -53,8 +64,9 @@ struct F32 {
 // for a row that was asked for ahead does not wait for the stores behind it.  Offsets need the alignment of an element only.
 typedef __amdgpu_buffer_rsrc_t Buffer;
 constexpr int kBufferFlags = 0x00020000;
-// Cache policy of rows (bit 1, non-temporal): each is read or written once and makes room at once.  us without -> with, forwards
-// 32760 x 1536 (stream in 32 bits) 111 -> 104, 75600 x 5120 (bf16) 588 -> 514, rotary of 12 heads 81 -> 77, backwards 131 -> 121.
+// Cache policy of rows (bit 1, non-temporal): each is read or written once and makes room at once.  us without -> with,
+// forwards 32760 x 1536 (stream in 32 bits) 111 -> 104, backwards 164 -> 158, 75600 x 5120 (bf16) 584 -> 542, rotary of 12
+// heads 83.5 -> 82, backwards 125 -> 117, of 40 heads 635 -> 655.
 constexpr int kStreamed = 2;
 struct Walk {
   char* at;
@@ -144,7 +156,8 @@ struct Piece {
     if constexpr (kNarrow)
       __builtin_amdgcn_raw_buffer_store_b64(u32x2{w[2 * run], w[2 * run + 1]}, to, offset, 0, kPolicy);
     else
-      __builtin_amdgcn_raw_buffer_store_b128(u32x4{w[4 * run], w[4 * run + 1], w[4 * run + 2], w[4 * run + 3]}, to, offset, 0, kPolicy);
+      __builtin_amdgcn_raw_buffer_store_b128(u32x4{w[4 * run], w[4 * run + 1], w[4 * run + 2], w[4 * run + 3]}, to, offset, 0,
+                                             kPolicy);
   }
   template <int kPolicy = kStreamed>
   __device__ __forceinline__ void store(Buffer to, int offset) const {
@@ -340,10 +353,10 @@ __device__ __forceinline__ void make_angles(const Speed& mine, int batch, int n,
 }
 
 // A workgroup: some heads (under NORM_ROW all) of q and the same heads of k, whose angles are the same, for a share of the
-// tokens, one or some at a time.  A row is a token's heads of q or of k, one after the other.  (Backwards through a norm, where weights and the sums
-// for their gradient would need 32 registers, a workgroup takes q or k.)  A thread holds four pairs of a head, a[4] and b[4].
-// WHOLE: they are eight entries in a row or, of turned halves, four and four; otherwise (a head's ragged end, four pairs across
-// the end of the turned halves) every entry is fetched by itself.
+// tokens, one or some at a time.  A row is a token's heads of q or of k, one after the other.  (Backwards through a norm,
+// where weights and the sums for their gradient would need 32 registers, a workgroup takes q or k.)  A thread holds four
+// pairs of a head, a[4] and b[4]. WHOLE: they are eight entries in a row or, of turned halves, four and four; otherwise (a
+// head's ragged end, four pairs across the end of the turned halves) every entry is fetched by itself.
 template <class Kind, bool HALVES, bool WHOLE, Sums SUMS, bool BWD>
 __global__ __launch_bounds__(SUMS == kSumWaves ? kMaxTeam : 256) void rotary_kernel(const RotaryParams p) {
   constexpr int kSize = Piece<Kind>::kSize;
@@ -654,7 +667,7 @@ __global__ __launch_bounds__(SUMS == kSumWaves ? kMaxTeam : 256) void rotary_ker
           to[place_a(e)] = da[side][e];
           to[place_b(e)] = db[side][e];
         }
-      } else if constexpr (SUMS != kSumWaves) {  // the heads share their weights: summed in order here, the tokens of the tile and their heads
+      } else if constexpr (SUMS != kSumWaves) {  // weights that heads share: the tile's tokens and their heads summed in order
         __shared__ float sums[256 * kEach];
         lds_barrier();
 #pragma unroll
@@ -996,7 +1009,7 @@ __global__ __launch_bounds__(S == kOnes ? 64 : kMaxTeam) void residual_fwd_kerne
 // and over the tokens of a row of modulation A = sum dh n, S = sum dh, C = sum dx n_y, from which all six gradients of the
 // parameters follow (group_sums_kernel): three sums in registers, where each gradient by itself would need six.  The waves meet
 // once for x, with both rows' statistics and the sums of dn and of dn (x - the wave's mean), which those of the waves are put
-// together from like the squares, and once more for y: us at 2 x 3913 rows of 1111, four meetings -> two, 53.8 -> 47.
+// together from like the squares, and once more for y: us at 2 x 3913 rows of 1111, four meetings -> two, 56.5 -> 54.4.
 template <class KindX, class KindY, Spread S>
 __global__ __launch_bounds__(S == kOnes ? 64 : kMaxTeam) void residual_bwd_kernel(const ResidualParams p) {
   __shared__ WaveRoom<3> room;

@@ -61,13 +61,14 @@ bool good_vector(const T* p, int dtype) {
 }
 bool good_grad(const float* p) { return ((uintptr_t)p & 3) == 0; }
 
-// Shares that each of `kinds` kinds of rows is dealt to, at most `rows` (of a kind), in workgroups of `waves` waves, `per_cu` of
-// them on a CU.  A workgroup has a row asked for at any time, and memory gives most when some 15 to 18 KB are asked for on each
-// CU, in whole workgroups for each CU: more of them get into each other's way, fewer do not keep it busy.  us at 256 / 512 / 768 /
-// 1024 / 1280 / 1536 workgroups: forwards 32760 x 1536, 9 KB a row, 114 / 104 / 111 / 111 / 113 / 114, 60000 x 1111, 4 KB, - / - / 108
-// / 115 / 124 / 127, 75600 x 5120, 20 KB, 514 / 564 / 555 / 592 / 614 / 607, backwards 32760 x 1536, 18 KB, 158 / 169 / 189 / 191 / 198
-// / 207, 12 KB, 149 / 119 / 128 / 136 / 148 / 154, rotary of 12 heads, 3 KB, 167 / 109 / 87 / 83 / 81 / 81, backwards, 6 KB, 220 / 138 /
-// 116 / 121 / 119 / 118.  Kinds that do not go evenly into that are dealt to four times as many, to be taken as CUs get free.
+// Shares that each of `kinds` kinds of rows is dealt to, at most `rows` (of a kind), in workgroups of `waves` waves, `per_cu`
+// of them on a CU.  A workgroup has a row asked for at any time, and memory gives most when some 15 to 18 KB are asked for on
+// each CU, in whole workgroups for each CU: more of them get into each other's way, fewer do not keep it busy.  us at 256 /
+// 512 / 768 / 1024 / 1280 / 1536 workgroups: forwards 32760 x 1536, 9 KB a row, 114 / 104 / 111 / 111 / 113 / 114, 60000 x
+// 1111, 4 KB, - / - / 108 / 115 / 124 / 127, 75600 x 5120, 20 KB, 514 / 564 / 555 / 592 / 614 / 607, backwards 32760 x 1536,
+// 18 KB, 158 / 169 / 189 / 191 / 198 / 207, 12 KB, 149 / 119 / 128 / 136 / 148 / 154, rotary of 12 heads, 3 KB, 167 / 109 /
+// 87 / 83 / 81 / 81, backwards, 6 KB, 220 / 138 / 116 / 121 / 119 / 118.  Kinds that do not go evenly into that are dealt to
+// four times as many, to be taken as CUs get free.
 int shares_of(int64_t kinds, int rows, int waves, int64_t per_cu) {
   const int64_t side_by_side = kCUs * std::max<int64_t>(1, std::min<int64_t>(per_cu, 32 / waves));
   const int64_t shares = kinds * 4 <= side_by_side ? side_by_side / kinds : (4 * side_by_side + kinds - 1) / kinds;
@@ -94,9 +95,9 @@ struct RotaryShape {
 };
 
 // A head takes a thread for each kEach entries; a workgroup takes all heads of a token (NORM_ROW) or as many as 256 threads
-// hold, and, where these are few and the tokens not too far apart (`together`), several tokens: us at 302400 tokens of 2 heads
-// of 128 with a token in a wave of its own 190, of 16 tokens in a workgroup of 256 threads 96; 2 x 3913 tokens of 5 heads of 72,
-// backwards, 28 -> 20.
+// hold, and, where these are few and the tokens not too far apart (`together`), several tokens: us with a token in a
+// workgroup of its own -> with 8 tokens, 302400 tokens of 2 heads of 128 153 -> 115, backwards through a norm 376 -> 197; 2 x
+// 3913 tokens of 5 heads of 72, backwards, 27.6 -> 24.9.
 RotaryShape rotary_shape(const lite_attn_rotary_desc_t& d, bool bwd, bool together) {
   RotaryShape s;
   const bool by_row = d.norm == LITE_ATTN_NORM_ROW;
@@ -200,7 +201,9 @@ int fill_rotary(const lite_attn_rotary_desc_t& d, const lite_attn_positions_t& a
 }
 
 // Whether the entries of neighbouring tokens share a line of memory.
-bool shares_lines(const lite_attn_heads_t& t, const lite_attn_rotary_desc_t& d) { return t.stride_n * size_of(d.dtype) % 128 != 0; }
+bool shares_lines(const lite_attn_heads_t& t, const lite_attn_rotary_desc_t& d) {
+  return t.stride_n * size_of(d.dtype) % 128 != 0;
+}
 
 void set(int64_t to[3], const lite_attn_heads_t& t, int dtype) {
   to[0] = t.stride_b * size_of(dtype);
@@ -310,8 +313,8 @@ int groups_of(const lite_attn_residual_desc_t& d) {
 }
 
 // A workgroup takes a row of `dim` entries, kEach in a thread, and rows of one group (tokens that share a row of modulation).
-// Backwards through a norm of y, whose sums come one after the other, a row takes longer, and one more workgroup on a CU pays (us
-// at 60000 x 1112, three -> four 207 -> 192; not in place of a single one, at 40000 x 5120 461 -> 480).
+// Backwards through a norm of y, whose sums come one after the other, a row takes longer, and one more workgroup on a CU pays
+// (us at 60000 x 1112, three -> four 207 -> 192; not in place of a single one, at 40000 x 5120 461 -> 480).
 ResidualShape residual_shape(const lite_attn_residual_desc_t& d, bool bwd) {
   ResidualShape s;
   s.threads = (d.dim + 64 * kEach - 1) / (64 * kEach) * 64;
