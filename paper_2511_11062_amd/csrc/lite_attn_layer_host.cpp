@@ -94,16 +94,35 @@ struct RotaryShape {
   int kinds;  // of workgroups of a batch entry
 };
 
-// A head takes a thread for each kEach entries; a workgroup takes all heads of a token (NORM_ROW) or as many as 256 threads
-// hold, and, where these are few and the tokens not too far apart (`together`), several tokens: us with a token in a
-// workgroup of its own -> with 8 tokens, 302400 tokens of 2 heads of 128 153 -> 115, backwards through a norm 376 -> 197; 2 x
-// 3913 tokens of 5 heads of 72, backwards, 27.6 -> 24.9.
-RotaryShape rotary_shape(const lite_attn_rotary_desc_t& d, bool bwd, bool together) {
+// How the tokens of a call may be taken: one by one, or several neighbouring ones, which must not lie too far apart; heads-first,
+// forwards, if these are neighbours in a result too.
+enum Taken { kOneByOne, kTogether, kHeadsFirst };
+
+// A head takes a thread for each kEach entries; a workgroup takes all heads of a token (NORM_ROW) or an even part of them, and,
+// where these are few, several tokens: us with a token in a workgroup of its own -> with 8 tokens, 302400 tokens of 2 heads of
+// 128 153 -> 115, backwards through a norm 376 -> 197; 2 x 3913 tokens of 5 heads of 72, backwards, 27.6 -> 24.9.
+// The part is what 256 threads hold; for results that are heads-first a quarter of that, so that there are four tokens or more
+// and what is written lies side by side in longer runs: us at 75600 tokens of 24 heads of 128 369 -> 337, of 64 195 -> 184, 20 of
+// 80 281 -> 205, 12 of 96 185 -> 146, 37 of 72 504 -> 372 (32 bits, 12 of 72 227 -> 234).  (Backwards the sums for the weights'
+// gradient would come in another order.)  And a smaller part where fewer than 0.72 of its threads have an entry and one more
+// split or a few give 0.9: 30 heads of 72 347 -> 280, 24 of 88 320 -> 252, backwards the same; from 0.75 to 0.98, 16 of 72, it is
+// 147 -> 151.
+RotaryShape rotary_shape(const lite_attn_rotary_desc_t& d, bool bwd, Taken taken) {
   RotaryShape s;
   const bool by_row = d.norm == LITE_ATTN_NORM_ROW;
   const int most = std::max(d.heads_q, d.heads_k);
   s.lanes = (d.head_dim + kEach - 1) / kEach;
-  s.team_heads = by_row ? most : std::min(most, std::max(1, 256 / s.lanes));
+  const int room = by_row ? most : std::max(1, (taken == kHeadsFirst ? 64 : 256) / s.lanes);
+  s.groups = (most + room - 1) / room;
+  if (!by_row && taken == kTogether) {
+    auto in_use = [&](int groups) {
+      const int row = (most + groups - 1) / groups * s.lanes, tokens = std::max(1, 256 / row);
+      return (double)most * s.lanes * tokens / (groups * ((tokens * row + 63) / 64 * 64));
+    };
+    for (int g = s.groups + 1; in_use(s.groups) < 0.72 && g <= std::min(most, s.groups + 4); ++g)
+      if (in_use(g) >= 0.9) s.groups = g;
+  }
+  s.team_heads = (most + s.groups - 1) / s.groups;
   s.groups = (most + s.team_heads - 1) / s.team_heads;
   s.row_lanes = s.team_heads * s.lanes;
   s.sum_log = 0;
@@ -121,7 +140,7 @@ RotaryShape rotary_shape(const lite_attn_rotary_desc_t& d, bool bwd, bool togeth
   } else {
     s.sums = kSumHeads;
   }
-  s.tokens = together && s.sums != kSumWaves ? std::max(1, std::min(256 / s.row_lanes, d.seqlen)) : 1;
+  s.tokens = taken != kOneByOne && s.sums != kSumWaves ? std::max(1, std::min(256 / s.row_lanes, d.seqlen)) : 1;
   s.threads = (s.tokens * s.row_lanes + 63) / 64 * 64;
   s.near_heads = s.tokens > 1 ? s.team_heads : std::min(s.team_heads, 64 % s.lanes ? 63 / s.lanes + 2 : 64 / s.lanes);
   s.kinds = s.groups * (rotary_sides(d.norm != LITE_ATTN_NORM_NONE, bwd) == 1 && d.heads_k ? 2 : 1);
@@ -131,6 +150,9 @@ RotaryShape rotary_shape(const lite_attn_rotary_desc_t& d, bool bwd, bool togeth
                        (18432 + bytes - 1) / bytes);
   return s;
 }
+
+// Whether neighbouring tokens of a head lie next to each other.
+bool heads_first(const lite_attn_heads_t& t) { return t.stride_n < t.stride_h; }
 
 // Whether what a workgroup (a wave, if it takes one token at a time) has of a tensor lies within 4 GiB: offsets have 32 bits.
 bool near(const lite_attn_heads_t& t, const lite_attn_rotary_desc_t& d, const RotaryShape& s, int heads) {
@@ -238,10 +260,11 @@ int check_rotary(const lite_attn_rotary_desc_t* d) {
 int plan_rotary(const lite_attn_rotary_desc_t& d, const lite_attn_rotary_fwd_t& a, RotaryParams* p, LayerLaunch* l) {
   const int heads[2] = {d.heads_q, d.heads_k}, sides = d.heads_k ? 2 : 1;
   const lite_attn_heads_t in[2] = {a.q, a.k}, out[2] = {a.q_out, a.k_out};
-  RotaryShape s = rotary_shape(d, false, true);
+  const bool first = heads_first(out[0]) || (sides == 2 && heads_first(out[1]));
+  RotaryShape s = rotary_shape(d, false, first ? kHeadsFirst : kTogether);
   for (int x = 0; x < sides; ++x) {
     if (!good(view(in[x], d, heads[x]), false) || !good(view(out[x], d, heads[x]), true)) return LITE_ATTN_EINVAL;
-    if (!near(in[x], d, s, heads[x]) || !near(out[x], d, s, heads[x])) s = rotary_shape(d, false, false);
+    if (!near(in[x], d, s, heads[x]) || !near(out[x], d, s, heads[x])) s = rotary_shape(d, false, kOneByOne);
   }
   for (int x = 0; x < sides; ++x)
     if (!near(in[x], d, s, heads[x]) || !near(out[x], d, s, heads[x])) return LITE_ATTN_EUNSUPPORTED;
@@ -265,14 +288,14 @@ int plan_rotary(const lite_attn_rotary_desc_t& d, const lite_attn_rotary_bwd_t& 
   const lite_attn_heads_t in[2] = {a.q, a.k}, g[2] = {a.dq_out, a.dk_out}, out[2] = {a.dq, a.dk};
   float* const grads[2] = {a.dq_weight, a.dk_weight};
   const bool normed = d.norm != LITE_ATTN_NORM_NONE;
-  RotaryShape s = rotary_shape(d, true, true);
+  RotaryShape s = rotary_shape(d, true, kTogether);
   auto all_near = [&](int x) {
     return (!normed || near(in[x], d, s, heads[x])) && near(g[x], d, s, heads[x]) && near(out[x], d, s, heads[x]);
   };
   for (int x = 0; x < sides; ++x) {
     if (normed && !good(view(in[x], d, heads[x]), false)) return LITE_ATTN_EINVAL;
     if (!good(view(g[x], d, heads[x]), false) || !good(view(out[x], d, heads[x]), true)) return LITE_ATTN_EINVAL;
-    if (!all_near(x)) s = rotary_shape(d, true, false);
+    if (!all_near(x)) s = rotary_shape(d, true, kOneByOne);
   }
   for (int x = 0; x < sides; ++x)
     if (!all_near(x)) return LITE_ATTN_EUNSUPPORTED;
@@ -435,8 +458,8 @@ extern "C" {
 size_t lite_attn_rotary_bwd_workspace(const lite_attn_rotary_desc_t* desc) {
   if (la::check_rotary(desc) != LITE_ATTN_OK || desc->norm == LITE_ATTN_NORM_NONE) return 0;
   // (which of the two shapes a call takes depends on its strides)
-  return std::max(la::rotary_workspace(*desc, la::rotary_shape(*desc, true, true)),
-                  la::rotary_workspace(*desc, la::rotary_shape(*desc, true, false)));
+  return std::max(la::rotary_workspace(*desc, la::rotary_shape(*desc, true, la::kOneByOne)),
+                  la::rotary_workspace(*desc, la::rotary_shape(*desc, true, la::kTogether)));
 }
 
 size_t lite_attn_residual_norm_bwd_workspace(const lite_attn_residual_desc_t* desc) {

@@ -216,6 +216,18 @@ def test_layouts_and_alignment(source, target, shift):
         c.check_backward()
 
 
+@pytest.mark.parametrize("heads,d,norm", [((30, 30), 72, "head"), ((37, 9), 72, "none"), ((24, 24), 128, "head"),
+                                          ((9, 20), 80, "head"), ((33, 33), 64, "none"), ((17, 3), 512, "head"),
+                                          ((12, 12), 90, "head"), ((70, 2), 6, "head")])
+@pytest.mark.parametrize("target", ["bhnd", "bnhd"])
+def test_heads_in_several_parts(heads, d, norm, target):
+    """More heads than a workgroup takes, in parts that do not come out even, of one token and of several."""
+    for dtype in ("bf16", "f32"):
+        c = Case(batch=2, heads=heads, d=d, grid=(3, 7, 11), text=6, norm=norm, target=target, dtype=dtype)
+        c.check_forward()
+        c.check_backward()
+
+
 def test_inputs_shared_by_batch_entries_and_heads():
     """Strides of 0: one key head for all, one batch entry for all."""
     c = Case(batch=3, heads=(4, 4), grid=(2, 3, 4), norm="row")
