@@ -12,10 +12,10 @@
 // this one, and keeps what belongs to its columns -- weights, gate, scale, shift, sums over tokens -- in registers all the while.
 // Sums over a row go through DPP inside a wave and once through LDS between waves.  Bytes that have to move, us and TB/s, where a
 // sum of two large tensors reaches 6.2 TB/s:
-//   rotary     40 heads of 128, 75600 tokens, norm over the token             3097 MB  655  4.7
+//   rotary     40 heads of 128, 75600 tokens, norm over the token             3097 MB  652  4.8
 //              12 heads, 32760 tokens                                          402 MB   82  4.9
 //              the same backwards                                              604 MB  117  5.2
-//   residual   75600 x 5120, both norms, a row of modulation for 3600 tokens  3097 MB  606  5.1
+//   residual   75600 x 5120, both norms, a row of modulation for 3600 tokens  3097 MB  599  5.2
 //              32760 x 1536, stream in 32 bits                                 604 MB  104  5.8
 //              the same backwards                                              906 MB  157  5.8
 #include <hip/hip_runtime.h>
